@@ -61,8 +61,10 @@ typedef enum {
   MOEV_W_FP32 = 0,         /* float32 */
   MOEV_W_BF16 = 1,         /* bfloat16 */
   MOEV_W_FP8E4M3_B128 = 2, /* e4m3fn codes + float32 scale per 128x128 block: W = code * s */
-  MOEV_W_MXFP4 = 3         /* e2m1 codes, two per byte (even k in the low nibble) + e8m0
+  MOEV_W_MXFP4 = 3,        /* e2m1 codes, two per byte (even k in the low nibble) + e8m0
                               scale per 32 along K: W = code * 2^(s-127) */
+  MOEV_W_INT4 = 4          /* moev_linear_w4 only: 4-bit integers, two per byte (even k in the low
+                              nibble) + bfloat16 scale per group along K: W = (code - 8) * s */
 } moev_wfmt;
 
 typedef enum { MOEV_ACT_FP32 = 0, MOEV_ACT_BF16 = 1 } moev_afmt;
@@ -328,6 +330,102 @@ moev_status moev_route_topk_static(const moev_config* cfg, const float* router_w
                                    int32_t gamma, int32_t* topk_ids, float* topk_w,
                                    void* cuda_stream);
 size_t moev_route_topk_static_scratch_floats(int32_t H, int32_t E, int32_t gamma);
+
+/* ======================================================================================
+ * The rest of a decoder block.  A verification pass (Sec. 5) runs, between two MoE layers, the
+ * residual addition and norm, the projections, and attention of the draft tree over the cached
+ * context; the paper takes these from its host framework.  The operators below are stateless like
+ * moev_select_drafts: no context, nothing allocated, nothing kept between calls, everything
+ * enqueued on cuda_stream of the current device, MOEV_EINVAL before anything is launched.  Row strides are in
+ * elements and are not looked at where a tensor has one row.
+ * ====================================================================================== */
+
+/* s = x + residual (binary32),  y = s / sqrt(mean(s^2) + eps) * w, and optionally the FP8 1x128
+ * quantisation of y (moev_act_quant), from the unrounded y.  residual_out receives s rounded to afmt.
+ * Outputs may be the inputs they replace (same pointer, stride and type).  Any H from 1 to 32768 and any stride >= H;
+ * rows on 16-byte boundaries with H a multiple of 8 are read and written by full vectors. */
+typedef struct {
+  int32_t n, H;
+  int32_t afmt;            /* moev_afmt of x, residual, residual_out, y */
+  int32_t wfmt;            /* moev_afmt of w */
+  float eps;
+  int32_t act_quant;       /* moev_act_quant; codes and scales are given exactly when it is not NONE */
+  const void* x;           /* [n, H] */
+  const void* residual;    /* [n, H] or NULL = 0 */
+  const void* w;           /* [H] */
+  void* residual_out;      /* [n, H] or NULL */
+  void* y;                 /* [n, H]; NULL allowed when codes are wanted only */
+  uint8_t* codes;          /* [n, H] e4m3 or NULL */
+  float* scales;           /* [n, ceil(H / 128)] or NULL */
+  int64_t x_stride, residual_stride, residual_out_stride, y_stride, codes_stride;
+} moev_norm;
+moev_status moev_add_rmsnorm(const moev_norm* p, void* cuda_stream);
+
+/* y [n, N] = x [n, K] W^T + bias for bf16 rows x and a 4-bit weight W [N, K] with group scales:
+ *   MOEV_W_INT4   codes uint8 [N, K / 2], scales bfloat16 [N, K / group], group 32, 64 or 128
+ *   MOEV_W_MXFP4  codes uint8 [N, K / 2], scales uint8 [N, K / 32], group 32
+ * K is a multiple of 32 and of group; N is free.  moev_w4_pack lays a weight out once in the order in
+ * which the kernel streams it (moev_w4_packed_bytes bytes, 16-byte aligned, caller-owned);
+ * moev_linear_w4 reads the packed form.  Products are exact, sums are binary32; y is yfmt (moev_afmt).
+ * Made for the few rows of a draft tree: more than 32 rows are taken 32 at a time, each pass reading the weight. */
+typedef struct {
+  int32_t N, K, wfmt, group;
+} moev_linear;
+size_t moev_w4_packed_bytes(const moev_linear* p); /* 0 for an invalid description */
+moev_status moev_w4_pack(const moev_linear* p, const void* codes, const void* scales, void* packed, void* cuda_stream);
+moev_status moev_linear_w4(const moev_linear* p, const void* packed, const float* bias /* [N] or NULL */, const void* x,
+                           int64_t x_stride, int32_t n, void* y, int64_t y_stride, int32_t yfmt, void* cuda_stream);
+
+/* Paged key / value cache in 8 bits.  value = code * scale, one scale per page and kv head for K and
+ * one for V, a power of two wherever moev_cache_append wrote it.
+ *   k [n_pages, n_kv_heads, page, head_dim] e4m3      v [n_pages, n_kv_heads, head_dim, page] e4m3
+ *   k_scale, v_scale [n_pages, n_kv_heads] float32
+ * page is 16, 32, 64 or 128, head_dim 64 or 128. */
+typedef struct {
+  int32_t n_pages, page, n_kv_heads, head_dim;
+  uint8_t *k, *v;
+  float *k_scale, *v_scale;
+} moev_kv_cache;
+
+/* The drafts of one call.  Sequence b has the token rows cu[b] .. cu[b+1] - 1 (its drafts, in an
+ * order in which parents come first) and ctx_len[b] tokens in the cache before them; its page c is
+ * page_table[b * table_cols + c]; draft i lives in slot ctx_len[b] + i.  parent [n_tokens]: index of a
+ * draft's parent within its sequence, -1 (or anything that is not an earlier draft) for one that
+ * continues the context; the position of a draft is ctx_len[b] + the number of its ancestors.  NULL:
+ * a chain, draft i continues draft i - 1.  A sequence may have no draft or no context.
+ *   max_drafts >= every sequence's drafts (<= 1024 with parents), max_len >= every ctx_len + drafts:
+ * host bounds that size the launches.  The arrays are device data: a sequence that breaks the bounds is
+ * left out, a page id outside the pool hides its keys, and both set *status (may be NULL; 1 sequence,
+ * 2 page id, 3 position behind the rotation table; never cleared).  Rows that belong to no sequence are
+ * left as they are. */
+typedef struct {
+  int32_t n_seq, n_tokens, max_drafts, max_len, table_cols;
+  const int32_t *cu, *ctx_len, *page_table, *parent;
+  int32_t* status;
+} moev_draft_batch;
+
+/* Write the drafts' keys and values (bf16 [n_tokens, n_kv_heads * head_dim], row strides multiples of 8
+ * elements) to the cache.  rope [rope_rows, head_dim] float32 (head_dim / 2 cosines, then as many sines,
+ * by position), or NULL for no rotation: dimensions i and i + head_dim / 2 of K, and of q where it is
+ * given, are rotated in binary32; q_out (may be q) receives the queries in bf16.  A page's scale is the smallest power of
+ * two that brings its largest magnitude to 448 or less; a page that held tokens before (ctx_len inside it) keeps
+ * the larger of that and its old scale, and its tokens are rescaled when it grows.  The pages that receive tokens belong to
+ * one sequence each.  A NaN stays NaN, an infinity becomes the largest finite value. */
+moev_status moev_cache_append(const moev_kv_cache* cache, const moev_draft_batch* batch, const void* k, int64_t k_stride,
+                              const void* v, int64_t v_stride, const float* rope, int32_t rope_rows, const void* q,
+                              int64_t q_stride, int32_t n_heads, void* q_out, int64_t q_out_stride, void* cuda_stream);
+
+/* Attention of the drafts over the cache (their own keys are in it).  q, out bf16 [n_tokens, n_heads *
+ * head_dim], n_heads a multiple of n_kv_heads (query head h reads kv head h / (n_heads / n_kv_heads)).
+ * A draft sees the context and, of the drafts, itself and its ancestors; with window > 0 of all these
+ * only the last window positions.  scores are multiplied by scale (> 0); sinks [n_heads] float32 (or
+ * NULL) join the denominator.  lse [n_tokens, n_heads] float32 (or NULL): natural log of the denominator.
+ * workspace: moev_cache_attend_workspace bytes for the same sizes (16-byte aligned; 0 = none needed);
+ * its contents do not matter before a call or after it, but calls that may overlap need one each. */
+size_t moev_cache_attend_workspace(const moev_kv_cache* cache, const moev_draft_batch* batch, int32_t n_heads, int32_t window);
+moev_status moev_cache_attend(const moev_kv_cache* cache, const moev_draft_batch* batch, const void* q, int64_t q_stride,
+                              int32_t n_heads, float scale, int32_t window, const float* sinks, void* out,
+                              int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 #ifdef __cplusplus
 }

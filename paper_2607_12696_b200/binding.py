@@ -10,7 +10,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libmoev.so")
 
-W_FP32, W_BF16, W_FP8E4M3_B128, W_MXFP4 = 0, 1, 2, 3
+W_FP32, W_BF16, W_FP8E4M3_B128, W_MXFP4, W_INT4 = 0, 1, 2, 3, 4
 ACT_FP32, ACT_BF16 = 0, 1
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 IMPL_AUTO, IMPL_SIMT, IMPL_TCGEN05 = 0, 1, 2
@@ -22,7 +22,8 @@ EXPORTS = ("moev_create", "moev_destroy", "moev_verify", "moev_verify_host", "mo
            "moev_launches_per_call", "moev_resolved_impl", "moev_profile_enable",
            "moev_profile_read", "moev_route_topk_static", "moev_route_topk_static_scratch_floats", "moev_select_drafts",
            "moev_verify_pipeline", "moev_prefetch_enable", "moev_verify_chain", "moev_ffn_span_enable",
-           "moev_ffn_span_read")
+           "moev_ffn_span_read", "moev_add_rmsnorm", "moev_w4_packed_bytes", "moev_w4_pack", "moev_linear_w4", "moev_cache_append",
+           "moev_cache_attend_workspace", "moev_cache_attend")
 
 
 class MoevError(RuntimeError):
@@ -54,6 +55,26 @@ class _Layer(C.Structure):
 
 class _Out(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in _OUT_FIELDS]
+
+
+class _Norm(C.Structure):
+    _fields_ = [("n", C.c_int32), ("H", C.c_int32), ("afmt", C.c_int32), ("wfmt", C.c_int32), ("eps", C.c_float), ("act_quant", C.c_int32)] + \
+               [(n, C.c_void_p) for n in ("x", "residual", "w", "residual_out", "y", "codes", "scales")] + \
+               [(n, C.c_int64) for n in ("x_stride", "residual_stride", "residual_out_stride", "y_stride", "codes_stride")]
+
+
+class _Linear(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("N", "K", "wfmt", "group")]
+
+
+class _KvCache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_pages", "page", "n_kv_heads", "head_dim")] + \
+               [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class _DraftBatch(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seq", "n_tokens", "max_drafts", "max_len", "table_cols")] + \
+               [(n, C.c_void_p) for n in ("cu", "ctx_len", "page_table", "parent", "status")]
 
 
 @dataclass
@@ -142,6 +163,22 @@ def lib() -> C.CDLL:
         L.moev_select_drafts.restype = C.c_int
         L.moev_select_drafts.argtypes = [C.c_int32, C.c_int32] + [C.c_void_p] * 4 + [C.c_int32, C.c_float, C.c_int32] + \
                                         [C.c_void_p] * 6
+        vp, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
+        L.moev_add_rmsnorm.restype = C.c_int
+        L.moev_add_rmsnorm.argtypes = [C.POINTER(_Norm), vp]
+        L.moev_w4_packed_bytes.restype = C.c_size_t
+        L.moev_w4_packed_bytes.argtypes = [C.POINTER(_Linear)]
+        L.moev_w4_pack.restype = C.c_int
+        L.moev_w4_pack.argtypes = [C.POINTER(_Linear), vp, vp, vp, vp]
+        L.moev_linear_w4.restype = C.c_int
+        L.moev_linear_w4.argtypes = [C.POINTER(_Linear), vp, vp, vp, i64, i32, vp, i64, i32, vp]
+        L.moev_cache_append.restype = C.c_int
+        L.moev_cache_append.argtypes = [C.POINTER(_KvCache), C.POINTER(_DraftBatch), vp, i64, vp, i64, vp, i32, vp, i64, i32, vp, i64, vp]
+        L.moev_cache_attend_workspace.restype = C.c_size_t
+        L.moev_cache_attend_workspace.argtypes = [C.POINTER(_KvCache), C.POINTER(_DraftBatch), i32, i32]
+        L.moev_cache_attend.restype = C.c_int
+        L.moev_cache_attend.argtypes = [C.POINTER(_KvCache), C.POINTER(_DraftBatch), vp, i64, i32, C.c_float, i32, vp, vp, i64, vp, vp,
+                                        C.c_size_t, vp]
         _lib = L
     return _lib
 

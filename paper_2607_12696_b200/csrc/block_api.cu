@@ -1,0 +1,353 @@
+// Host side of the operators around the MoE layer (the second part of include/moev.h): argument
+// checks, launch rules, launches.  Stateless: no context, nothing allocated, nothing kept.
+#include <algorithm>
+#include <cstdio>
+
+#include "attend.cuh"
+#include "common.cuh"
+#include "kv_cache.cuh"
+#include "linear_w4.cuh"
+#include "norm.cuh"
+
+using namespace moev;
+
+namespace {
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+int sm_count() {
+  static int n[64] = {};  // by device; a constant of the hardware
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+  if (n[dev] == 0 && cudaDeviceGetAttribute(&n[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
+  return n[dev];
+}
+
+// Dependent launch: the kernel may become resident while its predecessor drains; it waits (griddepcontrol.wait) before
+// it reads anything.
+template <typename... KArgs, typename... Args>
+cudaError_t launch(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
+}
+moev_status done(cudaError_t e) {
+  if (e == cudaSuccess) return MOEV_OK;
+  cudaGetLastError();
+  return MOEV_ECUDA;
+}
+
+// ---------------------------------------------------------------- norm
+template <typename T, typename TW, bool VEC>
+cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
+  // pieces of 8 columns: one per thread up to 4096 columns, else the fewest of 1, 2, 4, 8 that 512 threads can hold
+  const int pieces = (a.H + 7) / 8;
+  const int pv = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : pieces <= 2048 ? 4 : 8;
+  int threads = ((pieces + pv - 1) / pv + 31) & ~31;
+  const dim3 grid((unsigned)a.n);
+  switch (pv) {
+    case 1: return launch(add_rmsnorm_kernel<T, TW, 1, VEC>, grid, dim3(threads), 0, st, a);
+    case 2: return launch(add_rmsnorm_kernel<T, TW, 2, VEC>, grid, dim3(threads), 0, st, a);
+    case 4: return launch(add_rmsnorm_kernel<T, TW, 4, VEC>, grid, dim3(threads), 0, st, a);
+    default: return launch(add_rmsnorm_kernel<T, TW, 8, VEC>, grid, dim3(threads), 0, st, a);
+  }
+}
+template <typename T, typename TW>
+cudaError_t launch_norm_v(const NormArgs& a, bool vec, cudaStream_t st) {
+  return vec ? launch_norm<T, TW, true>(a, st) : launch_norm<T, TW, false>(a, st);
+}
+
+// ---------------------------------------------------------------- 4-bit linear
+bool linear_ok(const moev_linear* p) {
+  if (!p || p->N < 1 || p->K < 32 || p->K % 32 || p->K > (1 << 20)) return false;
+  if (p->wfmt == MOEV_W_MXFP4) return p->group == 32;
+  return p->wfmt == MOEV_W_INT4 && (p->group == 32 || p->group == 64 || p->group == 128) && p->K % p->group == 0;
+}
+size_t linear_tiles(const moev_linear* p) { return ((size_t)p->N + 15) / 16; }
+int linear_chunks(const moev_linear* p) { return (p->K + w4::kChunk - 1) / w4::kChunk; }
+int linear_scale_bytes(const moev_linear* p) {  // per tile and chunk
+  return p->wfmt == MOEV_W_MXFP4 ? 64 : 16 * (128 / p->group) * 2;
+}
+
+template <int FMT, int GB, int NT>
+cudaError_t launch_linear(const w4::Args& a0, cudaStream_t st) {
+  w4::Args a = a0;
+  const int sms = sm_count();
+  const int tiles = (a.N + 15) / 16;
+  const int rows = std::min(a.n, 8 * NT), passes = (a.n + 8 * NT - 1) / (8 * NT);
+  // Warps: all 16 of an SM share one copy of x.  kw of them share a tile's K: as many as it takes to give every
+  // warp of the machine work, at least 8 row groups per CTA otherwise, and never more than there are chunks.
+  int warps = 16, kw = 16;
+  while (kw > 1 && (kw > a.n_chunks || (tiles * kw) / 16 >= 8 * sms)) kw /= 2;
+  // few tiles: two smaller CTAs per SM start and end independently of each other
+  if (kw == 16 && tiles > sms && tiles <= 2 * sms) { warps = 8; kw = 8; }
+  size_t red = (size_t)warps * NT * 8 * 17 * 4, budget = 227 * 1024 - (kw > 1 ? red : 0);
+  const size_t whole = (size_t)rows * ((size_t)a.n_chunks * 256 + 64);
+  a.n_bufs = whole <= budget ? 1 : 2;
+  int piece = a.n_chunks;
+  if (a.n_bufs == 2) {  // x in two pieces at a time, each of at least one chunk per warp of a tile
+    piece = (int)((budget / 2 / rows - 64) / 256);
+    while (kw > piece) kw /= 2;
+    piece = piece / kw * kw;
+  }
+  if (kw == 1) red = 0;
+  const int rw = warps / kw;
+  a.kw = kw;
+  a.n_groups = (tiles + rw - 1) / rw;
+  a.phase_chunks = a.n_bufs == 1 ? (a.n_chunks + kw - 1) / kw * kw : piece;
+  a.x_pitch = piece * 256 + 64;
+  const size_t smem = (size_t)a.n_bufs * rows * a.x_pitch + red;
+  const int per_sm = smem <= 100 * 1024 && warps == 8 ? 2 : 1;
+  const int grid = std::min(a.n_groups, sms * per_sm);
+  return launch(w4::linear_w4_kernel<FMT, GB, NT>, dim3(grid, passes), dim3(warps * 32), smem, st, a);
+}
+template <int FMT, int GB>
+cudaError_t launch_linear_n(const w4::Args& a, cudaStream_t st) {
+  if (a.n <= 8) return launch_linear<FMT, GB, 1>(a, st);
+  if (a.n <= 16) return launch_linear<FMT, GB, 2>(a, st);
+  return launch_linear<FMT, GB, 4>(a, st);
+}
+
+// ---------------------------------------------------------------- cache
+bool batch_ok(const moev_kv_cache* c, const moev_draft_batch* d) {
+  if (!c || !d) return false;
+  if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 1024 || (c->head_dim != 64 && c->head_dim != 128)) return false;
+  if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return false;
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale || !aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 4) ||
+      !aligned(c->v_scale, 4))
+    return false;
+  if (d->n_seq < 0 || d->n_seq > 65535 || d->n_tokens < 0 || d->max_drafts < 1 || d->max_len < d->max_drafts || d->table_cols < 1) return false;
+  if (d->max_len > (1 << 30) || d->max_drafts > (1 << 24)) return false;
+  if (d->parent && d->max_drafts > kv::kMaxTree) return false;
+  return d->cu && d->ctx_len && d->page_table;
+}
+kv::Drafts drafts_of(const moev_draft_batch* d) {
+  return kv::Drafts{d->n_seq, d->n_tokens, d->max_drafts, d->max_len, d->table_cols, d->cu, d->ctx_len, d->page_table, d->parent, d->status};
+}
+kv::Cache cache_of(const moev_kv_cache* c) {
+  int lg = 4;
+  while ((1 << lg) < c->page) ++lg;
+  return kv::Cache{c->n_pages, lg, c->n_kv_heads, c->k, c->v, c->k_scale, c->v_scale};
+}
+
+struct Plan {
+  int wr, wk, row_tiles, chunks, chunk_keys;
+};
+Plan attend_plan(const moev_kv_cache* c, const moev_draft_batch* d, int n_heads, int window) {
+  Plan p;
+  const int rep = n_heads / c->n_kv_heads;
+  const long long rows = (long long)d->max_drafts * rep;
+  if (rows <= 16) { p.wr = 1; p.wk = 4; }
+  else if (rows <= 32) { p.wr = 2; p.wk = 4; }
+  else if (rows <= 64) { p.wr = 4; p.wk = 2; }
+  else { p.wr = 8; p.wk = 1; }
+  p.row_tiles = (int)((rows + 16 * p.wr - 1) / (16 * p.wr));
+  long long span = d->max_len;
+  if (window > 0) span = std::min<long long>(span, (long long)window + d->max_drafts + 63);
+  const long long base = (long long)std::max(1, d->n_seq) * c->n_kv_heads * p.row_tiles;
+  const int sms = sm_count();
+  // one wave of CTAs while that splits the keys at all; with many sequences or heads several waves, whose
+  // chunks even out their different lengths, but no chunk below 1024 keys
+  const int unit = 64 * p.wk;
+  long long want, least = unit;
+  if (base * 2 <= sms) want = sms / base;
+  else {
+    want = (8LL * sms + base - 1) / base;
+    least = 1024;
+  }
+  long long keys = std::max<long long>((span + want - 1) / want, least);
+  keys = (keys + unit - 1) / unit * unit;
+  p.chunk_keys = (int)keys;
+  p.chunks = (int)((span + keys - 1) / keys);
+  return p;
+}
+
+template <int D, int WR, int WK, int ST>
+cudaError_t launch_attend(const att::Args& a, cudaStream_t st) {
+  const int words = (a.d.max_drafts + 31) / 32;
+  const size_t smem = att::Cfg<D, WR, WK, ST>::smem(words, a.d.parent != nullptr);
+  return launch(att::attend_kernel<D, WR, WK, ST>, dim3(a.chunks, a.c.heads * a.row_tiles, a.d.n_seq), dim3(32 * WR * WK), smem, st, a);
+}
+template <int D>
+cudaError_t launch_attend_d(const att::Args& a, int wr, cudaStream_t st) {
+  cudaError_t e;
+  if (wr == 1) e = launch_attend<D, 1, 4, 3>(a, st);
+  else if (wr == 2) e = launch_attend<D, 2, 4, 3>(a, st);
+  else if (wr == 4) e = launch_attend<D, 4, 2, 4>(a, st);
+  else e = launch_attend<D, 8, 1, 3>(a, st);
+  if (e != cudaSuccess || a.chunks == 1) return e;
+  return launch(att::attend_combine_kernel<D>, dim3(a.d.max_drafts, (a.n_heads + 3) / 4, a.d.n_seq), dim3(128), 0, st, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+moev_status moev_add_rmsnorm(const moev_norm* p, void* cuda_stream) {
+  if (!p || p->n < 0 || p->H < 1 || p->H > 32768 || p->afmt < 0 || p->afmt > MOEV_ACT_BF16 || p->wfmt < 0 || p->wfmt > MOEV_ACT_BF16)
+    return MOEV_EINVAL;
+  if (p->act_quant < 0 || p->act_quant > MOEV_ACTQ_FP8_B128_POW2 || !(p->eps >= 0.f)) return MOEV_EINVAL;
+  if (!p->x || !p->w || (!p->y && !p->codes) || (p->act_quant != 0) != (p->codes != nullptr) || (p->codes != nullptr) != (p->scales != nullptr))
+    return MOEV_EINVAL;
+  const int es = p->afmt == MOEV_ACT_BF16 ? 2 : 4, ws = p->wfmt == MOEV_ACT_BF16 ? 2 : 4;
+  bool vec = p->H % 8 == 0 && aligned(p->w, 16) && aligned(p->codes, 8) && (!p->codes || p->codes_stride % 8 == 0);
+  const void* ptr[4] = {p->x, p->residual, p->y, p->residual_out};
+  const int64_t stride[4] = {p->x_stride, p->residual_stride, p->y_stride, p->residual_out_stride};
+  for (int i = 0; i < 4; ++i) {
+    if (!ptr[i]) continue;
+    if (!aligned(ptr[i], es) || (p->n > 1 && stride[i] < p->H)) return MOEV_EINVAL;
+    vec = vec && aligned(ptr[i], 16) && (stride[i] * es) % 16 == 0;
+  }
+  if (!aligned(p->w, ws) || !aligned(p->scales, 4) || (p->codes && p->n > 1 && p->codes_stride < p->H)) return MOEV_EINVAL;
+  if (p->n == 0) return MOEV_OK;
+  NormArgs a{p->x, p->residual, p->w, p->y, p->residual_out, p->codes, p->scales, p->x_stride, p->residual_stride, p->y_stride,
+             p->residual_out_stride, p->codes_stride, p->n, p->H, p->act_quant, p->eps};
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const bool xb = p->afmt == MOEV_ACT_BF16, wb = p->wfmt == MOEV_ACT_BF16;
+  cudaError_t e = xb ? (wb ? launch_norm_v<__nv_bfloat16, __nv_bfloat16>(a, vec, st) : launch_norm_v<__nv_bfloat16, float>(a, vec, st))
+                     : (wb ? launch_norm_v<float, __nv_bfloat16>(a, vec, st) : launch_norm_v<float, float>(a, vec, st));
+  return done(e);
+}
+
+size_t moev_w4_packed_bytes(const moev_linear* p) {
+  if (!linear_ok(p)) return 0;
+  return linear_tiles(p) * linear_chunks(p) * (size_t)(w4::kChunkBytes + linear_scale_bytes(p));
+}
+
+moev_status moev_w4_pack(const moev_linear* p, const void* codes, const void* scales, void* packed, void* cuda_stream) {
+  if (!linear_ok(p) || !codes || !scales || !packed || !aligned(codes, 16) || !aligned(scales, 16) || !aligned(packed, 16)) return MOEV_EINVAL;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const int chunks = linear_chunks(p);
+  const long long units = (long long)linear_tiles(p) * chunks;
+  const int fmt = p->wfmt == MOEV_W_INT4 ? w4::kInt4 : w4::kMx;
+  const long long words = units * 256;
+  uint8_t* sc = static_cast<uint8_t*>(packed) + units * w4::kChunkBytes;
+  w4::pack_codes_kernel<<<(unsigned)((words + 255) / 256), 256, 0, st>>>(static_cast<const uint8_t*>(codes), static_cast<uint32_t*>(packed),
+                                                                        p->N, p->K, chunks, fmt, words);
+  const int per_row = 128 / p->group;
+  const long long count = units * 16 * per_row;
+  const unsigned blocks = (unsigned)((count + 255) / 256);
+  if (fmt == w4::kInt4)
+    w4::pack_scales_kernel<uint16_t><<<blocks, 256, 0, st>>>(static_cast<const uint16_t*>(scales), reinterpret_cast<uint16_t*>(sc), p->N,
+                                                            p->K / p->group, chunks, per_row, count);
+  else
+    w4::pack_scales_kernel<uint8_t><<<blocks, 256, 0, st>>>(static_cast<const uint8_t*>(scales), sc, p->N, p->K / p->group, chunks, per_row, count);
+  return done(cudaGetLastError());
+}
+
+moev_status moev_linear_w4(const moev_linear* p, const void* packed, const float* bias, const void* x, int64_t x_stride, int32_t n, void* y,
+                           int64_t y_stride, int32_t yfmt, void* cuda_stream) {
+  if (!linear_ok(p) || !packed || !x || !y || n < 0 || yfmt < 0 || yfmt > MOEV_ACT_BF16) return MOEV_EINVAL;
+  if (!aligned(packed, 16) || !aligned(x, 2) || !aligned(y, yfmt == MOEV_ACT_BF16 ? 2 : 4) || !aligned(bias, 4)) return MOEV_EINVAL;
+  if (n > 1 && (x_stride < p->K || y_stride < p->N)) return MOEV_EINVAL;
+  if (n > 32 * 65535) return MOEV_EINVAL;
+  if (n == 0) return MOEV_OK;
+  w4::Args a{};
+  a.codes = static_cast<const uint8_t*>(packed);
+  a.n_chunks = linear_chunks(p);
+  a.scales = a.codes + linear_tiles(p) * a.n_chunks * (size_t)w4::kChunkBytes;
+  a.x = static_cast<const __nv_bfloat16*>(x);
+  a.bias = bias;
+  a.y = y;
+  a.x_stride = x_stride;
+  a.y_stride = y_stride;
+  a.n = n;
+  a.N = p->N;
+  a.K = p->K;
+  a.y_f32 = yfmt == MOEV_ACT_FP32;
+  a.x_vec = aligned(x, 16) && (n == 1 || x_stride % 8 == 0);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (p->wfmt == MOEV_W_MXFP4) return done(launch_linear_n<w4::kMx, 1>(a, st));
+  if (p->group == 32) return done(launch_linear_n<w4::kInt4, 1>(a, st));
+  if (p->group == 64) return done(launch_linear_n<w4::kInt4, 2>(a, st));
+  return done(launch_linear_n<w4::kInt4, 4>(a, st));
+}
+
+moev_status moev_cache_append(const moev_kv_cache* c, const moev_draft_batch* d, const void* k, int64_t k_stride, const void* v,
+                              int64_t v_stride, const float* rope, int32_t rope_rows, const void* q, int64_t q_stride, int32_t n_heads,
+                              void* q_out, int64_t q_out_stride, void* cuda_stream) {
+  if (!batch_ok(c, d) || !k || !v || !aligned(k, 16) || !aligned(v, 16) || k_stride % 8 || v_stride % 8) return MOEV_EINVAL;
+  const int64_t kv_row = (int64_t)c->n_kv_heads * c->head_dim;
+  if (d->n_tokens > 1 && (k_stride < kv_row || v_stride < kv_row)) return MOEV_EINVAL;
+  if (rope && (rope_rows < 1 || !aligned(rope, 16))) return MOEV_EINVAL;
+  if ((q != nullptr) != (q_out != nullptr)) return MOEV_EINVAL;
+  if (q) {
+    const int64_t q_row = (int64_t)n_heads * c->head_dim;
+    if (n_heads < 1 || n_heads % c->n_kv_heads || !aligned(q, 16) || !aligned(q_out, 16) || q_stride % 8 || q_out_stride % 8) return MOEV_EINVAL;
+    if (d->n_tokens > 1 && (q_stride < q_row || q_out_stride < q_row)) return MOEV_EINVAL;
+  }
+  if (d->n_seq == 0 || d->n_tokens == 0) return MOEV_OK;
+  kv::AppendArgs a{};
+  a.d = drafts_of(d);
+  a.c = cache_of(c);
+  a.k = static_cast<const __nv_bfloat16*>(k);
+  a.v = static_cast<const __nv_bfloat16*>(v);
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.q_out = static_cast<__nv_bfloat16*>(q_out);
+  a.k_stride = k_stride; a.v_stride = v_stride; a.q_stride = q_stride; a.q_out_stride = q_out_stride;
+  a.rope = rope;
+  a.rope_rows = rope_rows;
+  a.rep = q ? n_heads / c->n_kv_heads : 0;
+  // pages that max_drafts tokens can touch, wherever the first one falls in its page
+  const int pages = (d->max_drafts + c->page - 2) / c->page + 1;
+  const int n_par = d->parent && rope ? std::min(d->max_drafts, kv::kMaxTree) : 0;
+  const size_t smem = (size_t)(((c->page + n_par) * 4 + 15) & ~15) + (size_t)c->page * c->head_dim + (size_t)c->head_dim * (c->page + 4);
+  const dim3 grid(pages, c->n_kv_heads, d->n_seq);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return done(c->head_dim == 64 ? launch(kv::cache_append_kernel<64>, grid, dim3(256), smem, st, a)
+                                : launch(kv::cache_append_kernel<128>, grid, dim3(256), smem, st, a));
+}
+
+size_t moev_cache_attend_workspace(const moev_kv_cache* c, const moev_draft_batch* d, int32_t n_heads, int32_t window) {
+  if (!batch_ok(c, d) || n_heads < 1 || n_heads % c->n_kv_heads) return 0;
+  const Plan p = attend_plan(c, d, n_heads, window);
+  return p.chunks > 1 ? (size_t)p.chunks * d->n_tokens * n_heads * (c->head_dim + 2) * 4 : 0;
+}
+
+moev_status moev_cache_attend(const moev_kv_cache* c, const moev_draft_batch* d, const void* q, int64_t q_stride, int32_t n_heads, float scale,
+                              int32_t window, const float* sinks, void* out, int64_t out_stride, float* lse, void* workspace,
+                              size_t workspace_bytes, void* cuda_stream) {
+  if (!batch_ok(c, d) || !q || !out || n_heads < 1 || n_heads % c->n_kv_heads || window < 0 || !(scale > 0.f) || scale > 1e6f) return MOEV_EINVAL;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(sinks, 4) || q_stride % 8 || out_stride % 8) return MOEV_EINVAL;
+  const int64_t row = (int64_t)n_heads * c->head_dim;
+  if (d->n_tokens > 1 && (q_stride < row || out_stride < row)) return MOEV_EINVAL;
+  if (d->n_seq == 0 || d->n_tokens == 0) return MOEV_OK;
+  const Plan p = attend_plan(c, d, n_heads, window);
+  if ((long long)c->n_kv_heads * p.row_tiles > 65535 || (n_heads + 3) / 4 > 65535) return MOEV_EINVAL;
+  const size_t parts = (size_t)p.chunks * d->n_tokens * n_heads;
+  if (p.chunks > 1 && (!workspace || !aligned(workspace, 16) || workspace_bytes < parts * (c->head_dim + 2) * 4)) return MOEV_EINVAL;
+  att::Args a{};
+  a.d = drafts_of(d);
+  a.c = cache_of(c);
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.lse = lse;
+  a.sinks = sinks;
+  a.part_o = static_cast<float*>(workspace);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<float*>(workspace) + parts * c->head_dim);
+  a.q_stride = q_stride;
+  a.out_stride = out_stride;
+  a.n_heads = n_heads;
+  a.rep = n_heads / c->n_kv_heads;
+  a.row_tiles = p.row_tiles;
+  a.chunks = p.chunks;
+  a.chunk_keys = p.chunk_keys;
+  a.window = window;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return done(c->head_dim == 64 ? launch_attend_d<64>(a, p.wr, st) : launch_attend_d<128>(a, p.wr, st));
+}
+
+}  // extern "C"

@@ -1,0 +1,191 @@
+// Residual addition + root-mean-square norm, optionally with the FP8 1x128 quantisation of the result.
+//
+//   s = x + residual (binary32),  r = 1 / sqrt(mean(s^2) + eps),  y = s * r * w
+//   block of 128 columns: scale = act_scale(max |y|), code = e4m3(y / scale)   (common.cuh)
+//
+// The sum, the norm and the codes are taken from the unrounded binary32 values; what is written in
+// bf16 (the sum for the next layer, y) is rounded once, so neither rounding enters the other result.
+//
+// One CTA per row: a row is read once, into registers, and everything that follows works on those.
+// A thread owns pieces of 8 consecutive columns (one 16-byte access in bf16); 16 neighbouring
+// threads own one 128-column block, so its maximum is a butterfly over 16 lanes.  HBM bound for many
+// rows; for a few rows the time is one launch, one trip to memory and one block-wide reduction.
+#pragma once
+#include "common.cuh"
+
+namespace moev {
+
+struct NormArgs {
+  const void* x;
+  const void* res;
+  const void* w;
+  void* y;
+  void* res_out;
+  uint8_t* codes;
+  float* scales;
+  long long x_stride, res_stride, y_stride, res_out_stride, codes_stride;
+  int n, H, quant;
+  float eps;
+};
+
+template <typename T>
+__device__ __forceinline__ float to_float(T v);
+template <>
+__device__ __forceinline__ float to_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+// 8 consecutive values starting at column c; columns from H on read as zero
+template <typename T, bool VEC>
+__device__ __forceinline__ void norm_load8(const T* row, int c, int H, float (&v)[8]) {
+  if constexpr (VEC) {
+    if constexpr (sizeof(T) == 2) {
+      const uint4 q = *reinterpret_cast<const uint4*>(row + c);
+      const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(u[i] << 16);
+        v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+      }
+    } else {
+      const float4 a = *reinterpret_cast<const float4*>(row + c), b = *reinterpret_cast<const float4*>(row + c + 4);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c + i < H ? to_float(row[c + i]) : 0.f;
+  }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void norm_store8(T* row, int c, int H, const float (&v)[8]) {
+  if constexpr (VEC) {
+    if constexpr (sizeof(T) == 2) {
+      uint32_t u[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        u[i] = *reinterpret_cast<const uint32_t*>(&p);
+      }
+      *reinterpret_cast<uint4*>(row + c) = make_uint4(u[0], u[1], u[2], u[3]);
+    } else {
+      *reinterpret_cast<float4*>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<float4*>(row + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < H) {
+        if constexpr (sizeof(T) == 2) row[c + i] = __float2bfloat16_rn(v[i]);
+        else row[c + i] = v[i];
+      }
+  }
+}
+
+// PV pieces of 8 columns per thread (H <= PV * 8 * blockDim.x); VEC: every row of every tensor starts on a
+// 16-byte (codes: 8-byte) boundary and H is a multiple of 8.
+template <typename T, typename TW, int PV, bool VEC>
+__global__ void __launch_bounds__(512) add_rmsnorm_kernel(NormArgs a) {
+  __shared__ float part[16];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const long long row = blockIdx.x;
+  const int tid = threadIdx.x, H = a.H;
+  const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+  const T* res = a.res ? static_cast<const T*>(a.res) + row * a.res_stride : nullptr;
+  float v[PV][8];
+  float ss = 0.f;
+#pragma unroll
+  for (int p = 0; p < PV; ++p) {
+    const int c = (p * blockDim.x + tid) * 8;
+    if (c < H) norm_load8<T, VEC>(x, c, H, v[p]);
+    else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[p][i] = 0.f;
+    }
+  }
+  if (res) {
+    T* ro = a.res_out ? static_cast<T*>(a.res_out) + row * a.res_out_stride : nullptr;
+    float r[PV][8];
+#pragma unroll
+    for (int p = 0; p < PV; ++p) {
+      const int c = (p * blockDim.x + tid) * 8;
+      if (c < H) norm_load8<T, VEC>(res, c, H, r[p]);
+    }
+#pragma unroll
+    for (int p = 0; p < PV; ++p) {
+      const int c = (p * blockDim.x + tid) * 8;
+      if (c < H) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[p][i] += r[p][i];
+        if (ro) norm_store8<T, VEC>(ro, c, H, v[p]);
+      }
+    }
+  } else if (a.res_out) {
+    T* ro = static_cast<T*>(a.res_out) + row * a.res_out_stride;
+#pragma unroll
+    for (int p = 0; p < PV; ++p) {
+      const int c = (p * blockDim.x + tid) * 8;
+      if (c < H) norm_store8<T, VEC>(ro, c, H, v[p]);
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < PV; ++p)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ss = fmaf(v[p][i], v[p][i], ss);
+  ss = warp_sum(ss);
+  if ((tid & 31) == 0) part[tid >> 5] = ss;
+  __syncthreads();
+  float tot = 0.f;
+  for (int i = 0; i < (int)(blockDim.x >> 5); ++i) tot += part[i];  // same order in every thread
+  const float rs = 1.f / sqrtf(tot / (float)H + a.eps);
+
+  const TW* w = static_cast<const TW*>(a.w);
+  T* y = a.y ? static_cast<T*>(a.y) + row * a.y_stride : nullptr;
+#pragma unroll
+  for (int p = 0; p < PV; ++p) {
+    const int c = (p * blockDim.x + tid) * 8;
+    const bool in = c < H;
+    if (in) {
+      float g[8];
+      norm_load8<TW, VEC>(w, c, H, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[p][i] = v[p][i] * rs * g[i];
+      if (y) norm_store8<T, VEC>(y, c, H, v[p]);
+    }
+    if (a.quant && (c & ~127) < H) {  // the 16 lanes of a block decide alike
+      float m = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[p][i]));
+      const uint32_t lanes = 0xffffu << (tid & 16);
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(lanes, m, o));
+      const float s = act_scale(m, a.quant);
+      if (in) {
+        uint32_t q[2] = {0u, 0u};
+        if (a.quant == 2) {  // a power of two: the product with its reciprocal is the quotient, exactly
+          const float inv = 1.f / s;
+          if (s >= 1.17549435e-38f && inv >= 1.17549435e-38f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              q[i >> 2] |= (uint32_t)__nv_cvt_float_to_fp8(v[p][i] * inv, __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i >> 2] |= act_code(v[p][i], s) << (8 * (i & 3));
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) q[i >> 2] |= act_code(v[p][i], s) << (8 * (i & 3));
+        }
+        uint8_t* cr = a.codes + row * a.codes_stride;
+        if constexpr (VEC) *reinterpret_cast<uint2*>(cr + c) = make_uint2(q[0], q[1]);
+        else
+          for (int i = 0; i < 8; ++i)
+            if (c + i < H) cr[c + i] = (uint8_t)(q[i >> 2] >> (8 * (i & 3)));
+        if ((c & 127) == 0) a.scales[row * ((H + 127) / 128) + (c >> 7)] = s;
+      }
+    }
+  }
+}
+
+}  // namespace moev
