@@ -87,31 +87,39 @@ cudaError_t launch_linear(const w4::Args& a0, cudaStream_t st) {
   const int sms = sm_count();
   const int tiles = (a.N + 15) / 16;
   const int rows = std::min(a.n, 8 * NT), passes = (a.n + 8 * NT - 1) / (8 * NT);
-  // Warps: all 16 of an SM share one copy of x.  kw of them share a tile's K: as many as it takes to give every
-  // warp of the machine work, at least 8 row groups per CTA otherwise, and never more than there are chunks.
-  int warps = 16, kw = 16;
-  while (kw > 1 && (kw > a.n_chunks || (tiles * kw) / 16 >= 8 * sms)) kw /= 2;
-  // few tiles: two smaller CTAs per SM start and end independently of each other
-  if (kw == 16 && tiles > sms && tiles <= 2 * sms) { warps = 8; kw = 8; }
-  size_t red = (size_t)warps * NT * 8 * 17 * 4, budget = 227 * 1024 - (kw > 1 ? red : 0);
-  const size_t whole = (size_t)rows * ((size_t)a.n_chunks * 256 + 64);
-  a.n_bufs = whole <= budget ? 1 : 2;
-  int piece = a.n_chunks;
-  if (a.n_bufs == 2) {  // x in two pieces at a time, each of at least one chunk per warp of a tile
-    piece = (int)((budget / 2 / rows - 64) / 256);
-    while (kw > piece) kw /= 2;
-    piece = piece / kw * kw;
+  // All 16 warps of an SM share one copy of x.  kw of them share a tile's K: the fewest with which the tiles occupy
+  // most warps of the machine, never more than there are chunks.
+  const int warps = 16;
+  int kw = 1;
+  while (kw < 16 && 2 * kw <= a.n_chunks && tiles * kw * 10 < sms * warps * 6) kw *= 2;
+  // bytes of a piece of x: a row is 256 bytes a chunk + 64 (rows then start in alternating halves of the banks), a scale 2
+  auto piece_bytes = [&](int chunks) { return (size_t)rows * (chunks * 256 + 64) + (size_t)chunks * 16 * NT; };
+  const size_t most = 227 * 1024, red = (size_t)warps * NT * 8 * w4::kRedPitch * 4;
+  int grid, piece;
+  for (;; kw /= 2) {
+    const int rw = warps / kw;
+    grid = std::min((tiles + rw - 1) / rw, sms);
+    a.rounds = (tiles + rw * grid - 1) / (rw * grid);
+    const bool apart = kw > 1 && a.rounds > 1;  // x is needed again after the warps' sums have met
+    const size_t budget = most - (apart ? red : 0);
+    a.n_bufs = piece_bytes(a.n_chunks) <= budget ? 1 : 2;
+    piece = a.n_chunks;
+    if (a.n_bufs == 2) {  // two pieces at a time, each of at least one chunk per warp of a tile
+      piece = 1;
+      while (2 * piece_bytes(piece + 1) <= budget) ++piece;
+      if (piece < kw) continue;
+      piece = piece / kw * kw;
+    }
+    a.buf_bytes = (int)piece_bytes(piece);
+    a.red_at = apart ? a.n_bufs * a.buf_bytes : 0;
+    break;
   }
-  if (kw == 1) red = 0;
-  const int rw = warps / kw;
   a.kw = kw;
-  a.n_groups = (tiles + rw - 1) / rw;
   a.phase_chunks = a.n_bufs == 1 ? (a.n_chunks + kw - 1) / kw * kw : piece;
   a.x_pitch = piece * 256 + 64;
-  const size_t smem = (size_t)a.n_bufs * rows * a.x_pitch + red;
-  const int per_sm = smem <= 100 * 1024 && warps == 8 ? 2 : 1;
-  const int grid = std::min(a.n_groups, sms * per_sm);
-  return launch(w4::linear_w4_kernel<FMT, GB, NT>, dim3(grid, passes), dim3(warps * 32), smem, st, a);
+  const size_t smem = std::max((size_t)a.n_bufs * a.buf_bytes, a.red_at + (kw > 1 ? red : 0));
+  return a.n_bufs == 1 ? launch(w4::linear_w4_kernel<FMT, GB, NT, true>, dim3(grid, passes), dim3(warps * 32), smem, st, a)
+                       : launch(w4::linear_w4_kernel<FMT, GB, NT, false>, dim3(grid, passes), dim3(warps * 32), smem, st, a);
 }
 template <int FMT, int GB>
 cudaError_t launch_linear_n(const w4::Args& a, cudaStream_t st) {
@@ -223,7 +231,7 @@ moev_status moev_add_rmsnorm(const moev_norm* p, void* cuda_stream) {
 
 size_t moev_w4_packed_bytes(const moev_linear* p) {
   if (!linear_ok(p)) return 0;
-  return linear_tiles(p) * linear_chunks(p) * (size_t)(w4::kChunkBytes + linear_scale_bytes(p));
+  return linear_tiles(p) * linear_chunks(p) * (size_t)(w4::kChunkBytes + linear_scale_bytes(p)) + w4::kTailBytes;
 }
 
 moev_status moev_w4_pack(const moev_linear* p, const void* codes, const void* scales, void* packed, void* cuda_stream) {

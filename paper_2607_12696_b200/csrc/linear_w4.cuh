@@ -3,10 +3,13 @@
 //   INT4:  W[o, k] = (q[o, k] - 8) * s[o, k / group]     q in 0..15, s bf16, group 32, 64 or 128
 //   MXFP4: W[o, k] = e2m1(q[o, k]) * 2^(s[o, k / 32] - 127)
 //
-// The codes are exact in bf16, so the products with bf16 activations are exact too; mma.sync adds
-// them in binary32 over one group, the group's sum is multiplied by the binary32 scale and added to
-// the output's binary32 accumulator: no weight and no partial sum is rounded to fewer bits.
-// Bound by the weight stream (N K / 2 bytes + scales): 1.6 FLOP per byte and row of x.
+// mma.sync m16n8k16 with f16 operands and binary32 accumulators.  The codes are exact in f16.  x (bf16) is
+// brought to f16 by a power of two per row and chunk of 128 k, its largest element to [2^14, 2^15), so that an element
+// keeps all its 8 significant bits down to 2^-28 of the largest (and is off by at most 2^-40 of that below): the
+// products are exact.  They are added over one group, multiplied by the binary32 scale, added over the chunk, and
+// that is multiplied by the chunk's power of two and added to the output: no weight and no sum is rounded to fewer
+// bits.  f16 and not bf16 because its 10 mantissa bits take two code positions of a word each without a shift.
+// Bound by the weight stream (N K / 2 bytes + scales) and, close behind, by the instructions that unpack it.
 //
 // Packed layout (made once per weight, moev_w4_pack).  The weights are the A operand (16 outputs x
 // 16 k) and the tokens the B operand (8 columns), since a few tokens fill the narrow side.  A tile of
@@ -24,7 +27,9 @@ namespace w4 {
 
 constexpr int kInt4 = 0, kMx = 1;
 constexpr int kTileRows = 16, kChunk = 128, kChunkBytes = 1024;
+constexpr int kTailBytes = 4096;  // behind the packed weight: the last warp's ring reads up to three chunks too far
 constexpr int kDepth = 4;  // chunks a warp keeps in flight
+constexpr int kRedPitch = 20;  // floats per token where the warps' sums meet: lanes (g, t) write to 32 banks
 
 struct Args {
   const uint8_t* codes;   // packed
@@ -34,45 +39,64 @@ struct Args {
   void* y;
   long long x_stride, y_stride;
   int n, N, K, n_chunks;   // n: rows of x in all
-  int n_groups;            // row groups of RW tiles
+  int rounds;              // tiles per warp, one after another
   int kw;                  // warps that share a tile's K
   int phase_chunks;        // chunks of K per staged piece of x (a multiple of kw)
   int x_pitch;             // bytes per staged row
+  int buf_bytes;           // bytes per staged piece of x
+  int red_at;              // where the warps' sums meet: 0 = over x, when there is one round
   int n_bufs;              // 1: x is staged whole, 2: piece by piece
   int y_f32, x_vec;
 };
 
-// 8 codes of a word -> 4 bf16 pairs, pair p = k 2 p and 2 p + 1.
+// (w & MASK) | bits in one instruction
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "n"(MASK), "r"(bits));
+  return r;
+}
+
+// 8 codes of a word -> 4 f16 pairs, pair p = k 2 p and 2 p + 1.  MXFP4: 2^-14 times the value.
 template <int FMT>
-__device__ __forceinline__ void decode(uint32_t w, uint32_t (&r)[4]) {
+__device__ __forceinline__ void decode(uint32_t w, uint32_t magic, uint32_t (&r)[4]) {
   if constexpr (FMT == kInt4) {
-    // nibble p = k 2 p, nibble p + 4 = k 2 p + 1.  0x4300 | q is 128 + q in bf16; minus 136 is exact.
+    // nibble p = k 2 p, nibble p + 4 = k 2 p + 1.  0x6400 | q is 1024 + q and 0x6400 | q << 4 is 1024 + 16 q: one
+    // exact subtraction or fused multiply-add from q - 8.
+    const uint32_t v = w >> 8;
+    const uint32_t u[4] = {and_or<0x000F000Fu>(w, magic), and_or<0x00F000F0u>(w, magic), and_or<0x000F000Fu>(v, magic), and_or<0x00F000F0u>(v, magic)};
+    const __half2 off = __half2half2(__ushort_as_half(0x6408)), sixteenth = __half2half2(__ushort_as_half(0x2C00)),
+                  off16 = __half2half2(__ushort_as_half(0xD480));  // 1032, 1 / 16, -72
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-      const uint32_t u = ((w >> (4 * p)) & 0x000F000Fu) | 0x43004300u;
-      __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(&u);
-      v = __hsub2(v, __floats2bfloat162_rn(136.f, 136.f));
-      r[p] = *reinterpret_cast<uint32_t*>(&v);
+      __half2 h = *reinterpret_cast<const __half2*>(&u[p]);
+      h = p & 1 ? __hfma2(h, sixteenth, off16) : __hsub2(h, off);
+      r[p] = *reinterpret_cast<uint32_t*>(&h);
     }
   } else {
-    // magnitudes in order (nibble i = k i), looked up bytewise: {0, .5, 1, 1.5, 2, 3, 4, 6} as bf16; signs apart:
-    // bit 4 p + 3 that of k 2 p, bit 4 p + 19 that of k 2 p + 1.
-    const uint32_t s0 = w & 0x77777777u, s1 = s0 >> 16;
-    const uint32_t l0 = __byte_perm(0xC0800000u, 0xC0804000u, s0), h0 = __byte_perm(0x3F3F3F00u, 0x40404040u, s0);
-    const uint32_t l1 = __byte_perm(0xC0800000u, 0xC0804000u, s1), h1 = __byte_perm(0x3F3F3F00u, 0x40404040u, s1);
-    r[0] = __byte_perm(l0, h0, 0x5140) | ((w << 12) & 0x80008000u);
-    r[1] = __byte_perm(l0, h0, 0x7362) | ((w << 8) & 0x80008000u);
-    r[2] = __byte_perm(l1, h1, 0x5140) | ((w << 4) & 0x80008000u);
-    r[3] = __byte_perm(l1, h1, 0x7362) | (w & 0x80008000u);
+    // sign | e e m at bits 15 and 11..9 of f16 (subnormals included) is 2^-14 times the e2m1 value.  The packed halves
+    // hold pair 0 there, pair 1 three bits lower, the signs of 2 and 3 at 14 and 13, their magnitudes at 5..3 and 2..0.
+    r[0] = w & 0x8E008E00u;
+    r[1] = (w << 3) & 0x8E008E00u;
+    r[2] = and_or<0x0E000E00u>(w << 6, (w << 1) & 0x80008000u);
+    r[3] = and_or<0x0E000E00u>(w << 9, (w << 2) & 0x80008000u);
   }
 }
 
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// the same with a zero accumulator
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                              uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // GB: 32-k blocks per scale (1, 2, 4); MXFP4 has one byte per block.
@@ -91,185 +115,279 @@ struct Scales {
   __device__ __forceinline__ float get(int half, int i) const {
     const int at = half * kPerRow + i;
     if constexpr (FMT == kInt4) return bf16_bits_to_float((u[at >> 1] >> (16 * (at & 1))) & 0xffffu);
-    else return e8m0_to_float((u[at >> 2] >> (8 * (at & 3))) & 0xffu);
+    else return e8m0_to_float((u[at >> 2] >> (8 * (at & 3))) & 0xffu) * 16384.f;  // decode() leaves 2^-14
   }
 };
 
-// Stage columns [c0, c0 + cols) (cols a multiple of 128, columns from K on as zero) of rows [0, rows) of x.
-__device__ __forceinline__ void stage_x(const Args& a, const __nv_bfloat16* x, int rows, uint32_t dst, int c0, int cols) {
-  const int per = cols / 8;
-  for (int i = threadIdx.x; i < rows * per; i += blockDim.x) {
-    const int r = i / per, c = (i - r * per) * 8;
-    const uint32_t to = dst + (uint32_t)r * a.x_pitch + c * 2;
-    const __nv_bfloat16* from = x + (long long)r * a.x_stride + c0 + c;
-    if (c0 + c >= a.K) {  // K is a multiple of 32: a piece of 8 lies inside or outside
-      asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
-    } else if (a.x_vec) {
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-    } else {
-      uint32_t u[4];
+// Stage columns [c0, c0 + cols) (cols a multiple of 128, columns from K on as zero) of rows [0, rows) of x as f16, and
+// per chunk and row the power of two that undoes the scaling (bf16).  16 lanes own a row's chunk, 8 columns each.
+template <int NT>
+__device__ __forceinline__ void stage_x(const Args& a, const __nv_bfloat16* x, int rows, uint8_t* dst, uint16_t* back, int c0, int cols) {
+  const int lane = threadIdx.x & 31, half = threadIdx.x >> 4, halves = blockDim.x >> 4;
+  const uint32_t lanes = 0xffffu << (lane & 16);
+  const int chunks = cols >> 7;
+  constexpr int kBatch = NT == 1 ? 4 : 8;  // loads in flight per thread
+  int r = 0, ch = half;
+  while (ch >= chunks) { ch -= chunks; ++r; }
+  while (r < rows) {
+    uint32_t u[kBatch][4];
+    int rr[kBatch], cc[kBatch];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        u[j] = (uint32_t)__bfloat16_as_ushort(from[2 * j]) | ((uint32_t)__bfloat16_as_ushort(from[2 * j + 1]) << 16);
-      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]) : "memory");
+    for (int k = 0; k < kBatch; ++k) {
+      rr[k] = r;
+      cc[k] = ch;
+      const int c = ch * 128 + (lane & 15) * 8;
+      u[k][0] = u[k][1] = u[k][2] = u[k][3] = 0;
+      if (r < rows && c0 + c < a.K) {  // K is a multiple of 32: a piece of 8 lies inside or outside
+        const __nv_bfloat16* from = x + (long long)r * a.x_stride + c0 + c;
+        if (a.x_vec) {
+          const uint4 q = *reinterpret_cast<const uint4*>(from);
+          u[k][0] = q.x; u[k][1] = q.y; u[k][2] = q.z; u[k][3] = q.w;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            u[k][j] = (uint32_t)__bfloat16_as_ushort(from[2 * j]) | ((uint32_t)__bfloat16_as_ushort(from[2 * j + 1]) << 16);
+        }
+      }
+      ch += halves;
+      while (ch >= chunks) { ch -= chunks; ++r; }
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      if (rr[k] >= rows) break;
+      float v[8], m = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[2 * j] = __uint_as_float(u[k][j] << 16);
+        v[2 * j + 1] = __uint_as_float(u[k][j] & 0xffff0000u);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(v[j]));
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(lanes, m, o));
+      // 2^e <= m < 2^(e + 1): times 2^(14 - e), undone by 2^(e - 14).  Zero and tiny chunks as for e = -111; with an
+      // infinity among them the finite values stay finite
+      const int e = max((int)(__float_as_uint(m) >> 23) - 127, -111);
+      float up = __uint_as_float((uint32_t)(127 + 14 - min(e, 127)) << 23);
+      uint32_t down = (uint32_t)(127 + e - 14) << 7;
+      if (e > 127) {
+        up = 0x1p-113f;
+        down = (uint32_t)(127 + 113) << 7;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const __half2 h = __floats2half2_rn(v[2 * j] * up, v[2 * j + 1] * up);
+        u[k][j] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+      *reinterpret_cast<uint4*>(dst + rr[k] * a.x_pitch + (cc[k] * 128 + (lane & 15) * 8) * 2) = make_uint4(u[k][0], u[k][1], u[k][2], u[k][3]);
+      if ((lane & 15) == 0) back[cc[k] * (8 * NT) + rr[k]] = (uint16_t)down;
     }
   }
 }
 
-// CTA: blockDim / 32 warps = rw x kw; warp (r, k) takes tile r of the row group and every kw-th chunk of
-// K, beginning with chunk k.  Row groups go round the grid; the sums of the kw warps meet in shared
-// memory, in warp order.  Rows of x beyond 8 NT are the business of other blockIdx.y.
-template <int FMT, int GB, int NT>
+// CTA: blockDim / 32 warps = rw x kw; the kw warps of a tile take consecutive parts of its K.  Tiles go round all
+// CTAs first, then over a CTA's rw rows of warps, so that a last incomplete round leaves every SM the same work.  The
+// sums of the kw warps meet in shared memory, in warp order.  Rows of x beyond 8 NT are the business of other blockIdx.y.
+//
+// A warp walks over segments (one tile and one staged piece of x), each a run of consecutive chunks, in blocks of
+// kDepth chunks: the block's code is unrolled, with every address an immediate offset from one register per
+// operand, and behind each chunk's use the same registers are loaded with the chunk kDepth further on, across the
+// ends of segments.  The last block of a run loads past its end (into another warp's part, or the padding behind the
+// weight) and does not use it.
+template <int FMT, int GB, int NT, bool WHOLE>
 __global__ void __launch_bounds__(512, 1) linear_w4_kernel(const Args a) {
   extern __shared__ __align__(128) uint8_t smem[];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  using Sc = Scales<FMT, GB>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int warps = blockDim.x >> 5, kw_n = a.kw, rw_n = warps / kw_n;
   const int wk = warp % kw_n, wr = warp / kw_n;
   const int row0 = blockIdx.y * (8 * NT), rows = min(a.n - row0, 8 * NT);
   const __nv_bfloat16* x = a.x + (long long)row0 * a.x_stride;
   const int n_tiles = (a.N + kTileRows - 1) / kTileRows;
-  const int per_group = (a.n_chunks + kw_n - 1) / kw_n;  // chunks per warp and row group
-  const int groups = (a.n_groups - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
-  const int total = groups * per_group;
-  const uint32_t xs = (uint32_t)__cvta_generic_to_shared(smem);
-  const uint32_t buf_bytes = (uint32_t)rows * a.x_pitch;
-  float* red = reinterpret_cast<float*>(smem + (size_t)a.n_bufs * min(a.n, 8 * NT) * a.x_pitch);
-  using Sc = Scales<FMT, GB>;
+  const int tile0 = wr * (int)gridDim.x + (int)blockIdx.x, tile_step = rw_n * (int)gridDim.x;
+  const int n_phases = WHOLE ? 1 : (a.n_chunks + a.phase_chunks - 1) / a.phase_chunks;
+  const int items = a.phase_chunks / kw_n;           // chunks of a warp per segment, at most
+  const int blocks = (items + kDepth - 1) / kDepth;  // the same for every warp and segment
+  // a piece of x: rows, then its scales [chunk][8 NT]
+  const uint32_t buf_bytes = a.buf_bytes;
+  float* red = reinterpret_cast<float*>(smem + a.red_at);
 
-  // the i-th chunk of this warp
+  // chunks of this warp in a phase: the first one, and how many
+  auto first_of = [&](int phase) { return phase * a.phase_chunks + wk * items; };
+  auto count_of = [&](int phase) { return min(items, min(a.n_chunks, (phase + 1) * a.phase_chunks) - first_of(phase)); };
+
+  // ---- weights: a ring of kDepth chunks in registers
   uint4 wreg[kDepth][2];
   Sc sreg[kDepth];
-  auto fetch = [&](int i, uint4 (&w)[2], Sc& s) {
-    const int gi = i / per_group, c = (i - gi * per_group) * kw_n + wk;
-    const int tile = ((int)blockIdx.x + gi * (int)gridDim.x) * rw_n + wr;
-    if (i < total && c < a.n_chunks && tile < n_tiles) {
-      const size_t at = (size_t)tile * a.n_chunks + c;
-      const uint4* p = reinterpret_cast<const uint4*>(a.codes + at * kChunkBytes) + lane;
-      w[0] = __ldcs(p);
-      w[1] = __ldcs(p + 32);
-      s.load(a.scales + at * Sc::kBytes + g * Sc::kLane);
+  int f_round = 0, f_phase = 0, f_block = 0;
+  const uint8_t *f_w, *f_s;
+  auto f_seek = [&]() {  // to the segment (f_round, f_phase); to the start of the weight where that has no chunk
+    const int tile = tile0 + f_round * tile_step;
+    const bool on = tile < n_tiles && count_of(f_phase) > 0;
+    const size_t at = on ? (size_t)tile * a.n_chunks + first_of(f_phase) : 0;
+    f_w = a.codes + at * kChunkBytes + lane * 16;
+    f_s = a.scales + at * Sc::kBytes + g * Sc::kLane;
+  };
+  auto f_next = [&]() {  // one block on
+    if (++f_block < blocks) {
+      // a run that ends earlier than others' stays in its last blocks' place: nothing of it is used any more
+      if (f_block * kDepth < count_of(f_phase)) {
+        f_w += kDepth * kChunkBytes;
+        f_s += kDepth * Sc::kBytes;
+      }
+    } else {
+      f_block = 0;
+      if (++f_phase == n_phases) {
+        f_phase = 0;
+        ++f_round;
+      }
+      f_seek();
     }
+  };
+  auto fetch = [&](int d) {
+    const uint4* p = reinterpret_cast<const uint4*>(f_w + d * kChunkBytes);
+    wreg[d][0] = __ldcs(p);
+    wreg[d][1] = __ldcs(p + 32);
+    sreg[d].load(f_s + d * Sc::kBytes);
   };
 
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  f_seek();
 #pragma unroll
-  for (int d = 0; d < kDepth; ++d) fetch(d, wreg[d], sreg[d]);
-  const bool whole = a.n_bufs == 1;
-  const int n_phases = (a.n_chunks + a.phase_chunks - 1) / a.phase_chunks;
-  const int phase_items = a.phase_chunks / kw_n;
-  // piece number q of x (phase q % n_phases of row group q / n_phases) into buffer q & 1
-  auto stage = [&](int q) {
-    if (q < groups * n_phases) {
-      const int c0 = (q % n_phases) * a.phase_chunks;
-      const int nc = min(a.phase_chunks, a.n_chunks - c0);
-      stage_x(a, x, rows, xs + (whole ? 0u : (uint32_t)(q & 1) * buf_bytes), c0 * kChunk, nc * kChunk);
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  stage(0);
-  if (whole) {
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    __syncthreads();
-  }
+  for (int d = 0; d < kDepth; ++d) fetch(d);
+  f_next();
 
-  float acc[NT][4] = {};
-  int i = 0, j = 0, gi = 0, piece = 0;  // flat item, its place in the row group, row group, piece of x
-  const int b_row = min(g, rows - 1);
-  while (i < total) {
+  // ---- x: whole, or two pieces of K at a time
+  int s_phase = 0, s_left = a.rounds * n_phases, s_buf = 0;
+  auto stage = [&]() {  // the next piece, into the buffer that is free
+    if (s_left > 0) {
+      const int c0 = s_phase * a.phase_chunks;
+      uint8_t* to = smem + s_buf * buf_bytes;
+      stage_x<NT>(a, x, rows, to, reinterpret_cast<uint16_t*>(to + (size_t)rows * a.x_pitch), c0 * kChunk, min(a.phase_chunks, a.n_chunks - c0) * kChunk);
+      --s_left;
+      s_phase = s_phase + 1 == n_phases ? 0 : s_phase + 1;
+      s_buf ^= 1;
+    }
+  };
+  stage();
+  if (WHOLE) __syncthreads();
+  // this lane's rows of x (rows that are not there read another one's: their columns of the product are not used) and
+  // the scales of tokens 2 t and 2 t + 1
+  uint32_t xoff[NT];
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d, ++i) {
-      if (i >= total) break;
-      if (!whole && j % phase_items == 0) {
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        __syncthreads();  // the piece has landed, and everybody has left the other buffer
-        stage(piece + 1);
-        ++piece;
+  for (int q = 0; q < NT; ++q) xoff[q] = (uint32_t)min(q * 8 + g, rows - 1) * a.x_pitch + t * 16;
+  const uint32_t boff = (uint32_t)rows * a.x_pitch + t * 4;
+  uint32_t magic = 0x64006400u;
+  asm volatile("" : "+r"(magic));  // in a register, so that mask and or are one instruction
+
+  int buf = 1;
+  for (int round = 0; round < a.rounds; ++round) {
+    const int tile = tile0 + round * tile_step;
+    float acc[NT][4] = {};
+    for (int phase = 0; phase < n_phases; ++phase) {
+      if (!WHOLE) {
+        __syncthreads();  // the piece is there, and everybody has left the other buffer
+        stage();
+        buf ^= 1;
       }
-      const int c = j * kw_n + wk;
-      const int tile = ((int)blockIdx.x + gi * (int)gridDim.x) * rw_n + wr;
-      if (c < a.n_chunks && tile < n_tiles) {
-        const uint32_t base = xs + (whole ? 0u : (uint32_t)((piece - 1) & 1) * buf_bytes) +
-                              (uint32_t)((whole ? c : c % a.phase_chunks) * kChunk * 2 + t * 16);
-        const uint32_t word[8] = {wreg[d][0].x, wreg[d][0].y, wreg[d][0].z, wreg[d][0].w,
-                                  wreg[d][1].x, wreg[d][1].y, wreg[d][1].z, wreg[d][1].w};
+      int left = tile < n_tiles ? count_of(phase) : 0;
+      const uint8_t* piece = smem + (WHOLE ? 0u : buf * buf_bytes);
+      const uint8_t *xp[NT], *bp = piece + boff + wk * items * (16 * NT);
 #pragma unroll
-        for (int gr = 0; gr < 4 / GB; ++gr) {
-          float sum[NT][4] = {};
+      for (int q = 0; q < NT; ++q) xp[q] = piece + xoff[q] + wk * items * (kChunk * 2);
+      for (int block = 0; block < blocks; ++block) {
 #pragma unroll
-          for (int bb = 0; bb < GB; ++bb) {
-            const int b = gr * GB + bb;  // 32-k block of the chunk
-            uint32_t lo[4], hi[4];
-            decode<FMT>(word[2 * b], lo);
-            decode<FMT>(word[2 * b + 1], hi);
+        for (int d = 0; d < kDepth; ++d) {
+          if (d < left) {
+            const uint32_t word[8] = {wreg[d][0].x, wreg[d][0].y, wreg[d][0].z, wreg[d][0].w,
+                                      wreg[d][1].x, wreg[d][1].y, wreg[d][1].z, wreg[d][1].w};
+            float part[NT][4];  // the chunk's sums, in units of its tokens' powers of two
+#pragma unroll
+            for (int gr = 0; gr < 4 / GB; ++gr) {
+              float sum[NT][4];
+#pragma unroll
+              for (int bb = 0; bb < GB; ++bb) {
+                const int b = gr * GB + bb;  // 32-k block of the chunk
+                uint32_t lo[4], hi[4];
+                decode<FMT>(word[2 * b], magic, lo);
+                decode<FMT>(word[2 * b + 1], magic, hi);
+#pragma unroll
+                for (int q = 0; q < NT; ++q) {
+                  const uint4 xb = *reinterpret_cast<const uint4*>(xp[q] + d * (kChunk * 2) + b * 64);
+                  if (bb == 0) mma_f16_first(sum[q], lo[0], hi[0], lo[1], hi[1], xb.x, xb.y);
+                  else mma_f16(sum[q], lo[0], hi[0], lo[1], hi[1], xb.x, xb.y);
+                  mma_f16(sum[q], lo[2], hi[2], lo[3], hi[3], xb.z, xb.w);
+                }
+              }
+              const float s0 = sreg[d].get(0, gr), s1 = sreg[d].get(1, gr);
+#pragma unroll
+              for (int q = 0; q < NT; ++q)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  part[q][e] = gr == 0 ? (e < 2 ? s0 : s1) * sum[q][e] : fmaf(e < 2 ? s0 : s1, sum[q][e], part[q][e]);
+            }
 #pragma unroll
             for (int q = 0; q < NT; ++q) {
-              uint32_t b0, b1, b2, b3;
-              const uint32_t at = base + (uint32_t)(NT == 1 ? b_row : min(q * 8 + g, rows - 1)) * a.x_pitch + b * 64;
-              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b0), "=r"(b1), "=r"(b2), "=r"(b3) : "r"(at));
-              mma_bf16(sum[q], lo[0], hi[0], lo[1], hi[1], b0, b1);
-              mma_bf16(sum[q], lo[2], hi[2], lo[3], hi[3], b2, b3);
+              const uint32_t b = *reinterpret_cast<const uint32_t*>(bp + d * (16 * NT) + q * 16);
+              const float f0 = __uint_as_float(b << 16), f1 = __uint_as_float(b & 0xffff0000u);
+              acc[q][0] = fmaf(f0, part[q][0], acc[q][0]);
+              acc[q][1] = fmaf(f1, part[q][1], acc[q][1]);
+              acc[q][2] = fmaf(f0, part[q][2], acc[q][2]);
+              acc[q][3] = fmaf(f1, part[q][3], acc[q][3]);
             }
           }
-          const float s0 = sreg[d].get(0, gr), s1 = sreg[d].get(1, gr);
-#pragma unroll
-          for (int q = 0; q < NT; ++q) {
-            acc[q][0] = fmaf(s0, sum[q][0], acc[q][0]);
-            acc[q][1] = fmaf(s0, sum[q][1], acc[q][1]);
-            acc[q][2] = fmaf(s1, sum[q][2], acc[q][2]);
-            acc[q][3] = fmaf(s1, sum[q][3], acc[q][3]);
+          if (d & 1) {
+            fetch(d - 1);
+            fetch(d);
           }
         }
-      }
-      fetch(i + kDepth, wreg[d], sreg[d]);
-      if (++j == per_group) {
-        // the row group is done: lane (g, t) holds outputs g and g + 8 of the tile for tokens 2 t and 2 t + 1
-        if (kw_n == 1) {
+        f_next();
+        left -= kDepth;
+        bp += kDepth * 16 * NT;
 #pragma unroll
-          for (int q = 0; q < NT; ++q)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int o = tile * kTileRows + g + 8 * (e >> 1), r = q * 8 + 2 * t + (e & 1);
-              if (tile < n_tiles && o < a.N && r < rows) {
-                const float v = acc[q][e] + (a.bias ? a.bias[o] : 0.f);
-                const long long at = (long long)(row0 + r) * a.y_stride + o;
-                if (a.y_f32) static_cast<float*>(a.y)[at] = v;
-                else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
-              }
-            }
-        } else {
-          // [warp][token][output], 17 floats a token
-          float* mine = red + warp * (NT * 8 * 17);
-#pragma unroll
-          for (int q = 0; q < NT; ++q)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mine[(q * 8 + 2 * t + (e & 1)) * 17 + g + 8 * (e >> 1)] = acc[q][e];
-          __syncthreads();
-          const int first = ((int)blockIdx.x + gi * (int)gridDim.x) * rw_n * kTileRows;  // the group's first output
-          for (int z = threadIdx.x; z < rw_n * kTileRows * rows; z += blockDim.x) {
-            const int r = z / (rw_n * kTileRows), lo = z - r * (rw_n * kTileRows), o = first + lo;
-            if (o < a.N) {
-              const float* p = red + ((lo >> 4) * kw_n) * (NT * 8 * 17) + r * 17 + (lo & 15);
-              float v = 0.f;
-              for (int k = 0; k < kw_n; ++k) v += p[k * (NT * 8 * 17)];
-              v += a.bias ? a.bias[o] : 0.f;
-              const long long at = (long long)(row0 + r) * a.y_stride + o;
-              if (a.y_f32) static_cast<float*>(a.y)[at] = v;
-              else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
-            }
-          }
-          __syncthreads();
-        }
-#pragma unroll
-        for (int q = 0; q < NT; ++q)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[q][e] = 0.f;
-        j = 0;
-        ++gi;
+        for (int q = 0; q < NT; ++q) xp[q] += kDepth * kChunk * 2;
       }
     }
+    // lane (g, t) holds outputs g and g + 8 of the tile for tokens 2 t and 2 t + 1
+    if (kw_n == 1) {
+#pragma unroll
+      for (int q = 0; q < NT; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int o = tile * kTileRows + g + 8 * (e >> 1), r = q * 8 + 2 * t + (e & 1);
+          if (tile < n_tiles && o < a.N && r < rows) {
+            const float v = acc[q][e] + (a.bias ? a.bias[o] : 0.f);
+            const long long at = (long long)(row0 + r) * a.y_stride + o;
+            if (a.y_f32) static_cast<float*>(a.y)[at] = v;
+            else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
+          }
+        }
+    } else {
+      // [warp][token][output]
+      if (a.red_at == 0) __syncthreads();  // everybody is done with x
+      float* mine = red + warp * (NT * 8 * kRedPitch);
+#pragma unroll
+      for (int q = 0; q < NT; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine[(q * 8 + 2 * t + (e & 1)) * kRedPitch + g + 8 * (e >> 1)] = acc[q][e];
+      __syncthreads();
+      for (int z = threadIdx.x; z < rw_n * kTileRows * rows; z += blockDim.x) {
+        const int lo = z & 15, rr = z >> 4, w = rr % rw_n, r = rr / rw_n;
+        const int o = ((round * rw_n + w) * (int)gridDim.x + (int)blockIdx.x) * kTileRows + lo;
+        if (o < a.N) {
+          const float* p = red + w * kw_n * (NT * 8 * kRedPitch) + r * kRedPitch + lo;
+          float v = 0.f;
+          for (int k = 0; k < kw_n; ++k) v += p[k * (NT * 8 * kRedPitch)];
+          v += a.bias ? a.bias[o] : 0.f;
+          const long long at = (long long)(row0 + r) * a.y_stride + o;
+          if (a.y_f32) static_cast<float*>(a.y)[at] = v;
+          else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
+        }
+      }
+      if (round + 1 < a.rounds) __syncthreads();
+    }
   }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
 // One thread per packed word: tile, chunk, half h, lane 4 g + t, word {row g | g + 8} x {block 2 h | 2 h + 1}.
@@ -289,9 +407,15 @@ __global__ void pack_codes_kernel(const uint8_t* codes, uint32_t* out, int N, in
 #pragma unroll
     for (int p = 0; p < 4; ++p) r |= ((c >> (8 * p)) & 15u) << (4 * p) | ((c >> (8 * p + 4)) & 15u) << (4 * p + 16);
   } else {
-    r = c & 0x77777777u;
 #pragma unroll
-    for (int p = 0; p < 4; ++p) r |= ((c >> (8 * p + 3)) & 1u) << (4 * p + 3) | ((c >> (8 * p + 7)) & 1u) << (4 * p + 19);
+    for (int h = 0; h < 2; ++h) {  // half h: the odd or even k of each pair
+      uint32_t q[4];
+#pragma unroll
+      for (int p = 0; p < 4; ++p) q[p] = (c >> (8 * p + 4 * h)) & 15u;
+      const uint32_t v = (q[0] >> 3) << 15 | (q[0] & 7u) << 9 | (q[1] >> 3) << 12 | (q[1] & 7u) << 6 | (q[2] >> 3) << 14 |
+                         (q[3] >> 3) << 13 | (q[2] & 7u) << 3 | (q[3] & 7u);
+      r |= v << (16 * h);
+    }
   }
   out[z] = r;
 }
