@@ -1,29 +1,37 @@
-// Attention of draft tokens over the paged 8-bit cache (kv_cache.cuh).
+// Attention of draft tokens over the paged 8-bit cache (kv_cache.cuh), on the fifth-generation tensor cores.
 //
 //   score[r, j] = scale * q_r . k_j over the context's keys (the last `window` positions of them) and
 //   the draft's own ancestors and itself;  out_r = sum_j p[r, j] v_j,  p = softmax (with an optional
 //   sink logit per head in the denominator),  lse_r = log of the denominator + maximum.
 //
-// Rows of a tile are (draft, query head of one kv head): the heads that share keys share their loads.
-// mma.sync m16n8k16 with f16 operands and binary32 accumulators: an e4m3 code is exact in f16, q (bf16)
-// is brought to at most 2^14 by a power of two per row, where f16 holds all 8 of its significant bits
-// down to 2^-28 of the row's largest element, and the probabilities are rounded once to f16 (2^-11).
-// Codes go to the multiplier as they are: the scale of a page's K multiplies the scores, that of its
-// V the probabilities.  p * v_scale / u * 2^14, with u the largest V scale seen so far, uses f16's
-// range from 2^14 down, so a page whose scale is 2^-20 of the largest still keeps 8 bits or more.
+// Rows of a tile are (draft, query head of one kv head): the heads that share keys share their loads.  Both
+// products have the cache as the A operand of tcgen05.mma (128 wide whatever the rows) and the rows as the narrow
+// one, N = R = 16, 32, 64 or 128:
+//   S^T [128 keys, R]  = K tile [128 keys, D] . Q^T          O^T [D, R] += V^T tile [D, 128 keys] . P^T
+// so the e4m3 codes go from the cache by TMA to shared memory and from there to the multiplier as they are; a page
+// is stored in the order in which the instruction reads it (K by token, V by dimension), a tile is 128 / page pages
+// side by side, each in the swizzle of its row length.  kind::f8f6f4 wants 8-bit operands on both sides:
+//   q (bf16): three e4m3 terms of q * 2^e, largest element in [128, 256): each term takes the rest of the one before;
+//     what is left is 2^-18 of the row's largest element or 2^-12 of the element, whichever is more.  They add in one accumulator.
+//   p: two terms, hi = e4m3(p), lo = e4m3(16 (p - hi)), in accumulators of their own, O = O_hi + O_lo / 16: off by 2^-8
+//     of p at most (half a step of half a step; 7e-4 in the mean square, under bf16's own 1.7e-3 of the output) down to
+//     2^-12 of the row's maximum, and by 2^-20 of the maximum below that.
+// The scale of a page's K multiplies its scores, that of its V the probabilities relative to the largest V scale of late.
 //
-// Which key an MMA calls its n-th, and which dimension its k-th, is free as long as both operands agree.
-// Lane (g, t) = (lane / 4, lane % 4).  Scores: lane t's 16-byte piece t + 4 i of a key's row holds the
-// dimensions of four MMA steps; column n of key tile j is key 16 (n / 2) + 2 j + n % 2, so that lane t
-// ends up with the scores of the 16 consecutive keys 16 t .. 16 t + 15 of the 64: one page, one scale.  Second
-// product: lane t's 16 bytes of a V row are those 16 keys, four MMA steps of four, and its scores are
-// already in the A layout.  Both operands come out of shared memory by full 16-byte loads, no transposition.
+// In S^T a thread is a key (one page, one scale) and its registers are rows, so a maximum over keys would go across
+// lanes.  It is not taken: the reference m_r only has to be near it.  p = 2^(s - m_r) may reach 2^3 (times 2^5 it still
+// fits e4m3); only when some score exceeds that (always in the first tile, then rarely) the CTA takes the
+// maxima, moves m_r and rescales O and the denominators.  Those are per thread, summed across lanes once at the end.
 //
-// Work split: grid = (chunks of the key range, kv head x row tiles, sequence); the WK key groups of a
-// CTA take every WK-th tile of 64 keys of the chunk, its WR warps 16 rows each.  Key groups meet in shared
-// memory, chunks in a second kernel (attend_combine), both in fixed order.
+// Roles: one warp loads (TMA), one thread issues the MMAs, eight warps do the softmax, four for each half of the
+// rows (tensor memory gives a warp a quarter of the lanes).  S and P are double-buffered: S of tile i + 1 is
+// computed while the softmax works on tile i.  Work split: grid = (chunks of the key range, kv head x row tiles,
+// sequence); chunks meet in a second kernel (attend_combine), in order.  Every wait is bounded.
 #pragma once
+#include <cuda.h>
+
 #include "kv_cache.cuh"
+#include "ptx.cuh"
 
 namespace moev {
 namespace att {
@@ -32,7 +40,12 @@ using kv::Cache;
 using kv::Drafts;
 using kv::Seq;
 
-constexpr int kTile = 64;
+constexpr int kKeys = 128;                 // keys of a tile
+constexpr int kThreads = 320;              // 8 softmax warps, loader, MMA issuer
+constexpr float kLimit = 3.f;              // scores may exceed the reference by this many powers of two ...
+constexpr float kUp = 32.f, kDown = 1.f / 32.f;  // ... and p is kept times 2^5: 2^8 < 448
+constexpr float kUnseen = -3.0e38f;        // reference of a row that has not seen a key yet
+constexpr unsigned long long kBudgetNs = 2000000000ull;
 
 struct Args {
   Drafts d;
@@ -48,418 +61,592 @@ struct Args {
   float scale_log2;
 };
 
-__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// four e4m3 codes -> two f16 pairs
-__device__ __forceinline__ void codes_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
-      : "=r"(lo), "=r"(hi)
-      : "r"(w));
-}
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint4 lds128(uint32_t at) {
-  uint4 r;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(at));
+__device__ __forceinline__ float warp_max(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
 }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool on) {
-  const int n = on ? 16 : 0;  // 0: zeros
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+__device__ __forceinline__ bool any_of_256(bool v) {
+  int r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, 1, 256, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"((int)v)
+      : "memory");
+  return r != 0;
 }
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool on) {
-  const int n = on ? 4 : 0;
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]),
+               "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ptx::smem_u32(dst)), "l"(src),
+               "r"(bytes), "r"(ptx::smem_u32(bar))
+               : "memory");
+}
+// two f16 -> two e4m3 codes (saturating) and back
+__device__ __forceinline__ uint32_t f16_to_codes(uint32_t h) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
+  return r;
+}
+__device__ __forceinline__ uint32_t codes_to_f16(uint32_t c) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)c));
+  return r;
 }
 
-// First key of the range that a sequence's drafts can see (a multiple of 64).
+// First key of the range that a sequence's drafts can see (a multiple of 128).
 __device__ __forceinline__ int range_start(const Seq& s, int window) {
-  return window > 0 ? max(0, s.ctx + 1 - window) & ~(kTile - 1) : 0;
+  return window > 0 ? max(0, s.ctx + 1 - window) & ~(kKeys - 1) : 0;
 }
 
-template <int D, int WR, int WK, int ST>
+// Byte of 16-byte piece `seg` (16 keys) of dimension d in a V tile: pages side by side, each [D][page] with the swizzle
+// of its row length (128, 64 or 32 bytes; none for 16).
+template <int D>
+__device__ __forceinline__ uint32_t v_piece(int d, int seg, int page_log2) {
+  if (page_log2 == 7) return d * 128 + ((seg ^ (d & 7)) << 4);
+  if (page_log2 == 6) return (seg >> 2) * (D * 64) + d * 64 + (((seg & 3) ^ ((d >> 1) & 3)) << 4);
+  if (page_log2 == 5) return (seg >> 1) * (D * 32) + d * 32 + (((seg & 1) ^ ((d >> 2) & 1)) << 4);
+  return seg * (D * 16) + d * 16;
+}
+// Byte of element (row, d) of a K-major operand with rows of D bytes in the swizzle of that length.
+template <int D>
+__device__ __forceinline__ uint32_t q_byte(int r, int d) {
+  return D == 128 ? r * 128 + (((d >> 4) ^ (r & 7)) << 4) + (d & 15) : r * 64 + (((d >> 4) ^ ((r >> 1) & 3)) << 4) + (d & 15);
+}
+// upper half of a shared-memory matrix descriptor: stride between groups of 8 rows (bytes), layout type
+__device__ __forceinline__ uint64_t desc_of(uint32_t addr, uint32_t lead, uint32_t stride, uint32_t layout) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | (uint64_t)1 << 46 |
+         (uint64_t)layout << 61;
+}
+constexpr uint32_t kSw128 = 2, kSw64 = 4, kSw32 = 6, kSwNone = 0;
+
+template <int D, int R>
 struct Cfg {
-  static constexpr int kThreads = 32 * WR * WK;
-  static constexpr int kStage = 2 * kTile * D + 64;  // K [64][D], V [D][64], 4 + 4 scales, 4 flags: page in the pool
-  static constexpr int kRing = WK * ST * kStage;
-  static constexpr int kMerge = WK > 1 ? WR * WK * (16 * (D + 4) + 32) * 4 : 0;  // after the loop, over the ring
-  static constexpr int kMain = kRing > kMerge ? kRing : kMerge;
-  static size_t smem(int words, int tree) {  // + ancestor words, depths and parents of the tile's drafts
-    return kMain + (tree ? (size_t)(16 * WR) * (words + 1) * 4 + (size_t)words * 32 * 4 : 0);
-  }
+  static constexpr int kCtas = R <= 32 ? 2 : 1;  // per SM
+  static constexpr int kTile = kKeys * D;        // bytes of a K or V tile
+  static constexpr int kStages = D == 128 ? (R <= 32 ? 2 : R == 64 ? 4 : 3) : (R <= 32 ? 4 : 6);
+  static constexpr int kP = R * kKeys;           // bytes of one term of P
+  static constexpr int kQ = R * D;
+  static constexpr int kTmem = 4 * R;            // S x 2, O_hi, O_lo
+  // byte offsets
+  static constexpr int oK = 0, oV = kStages * kTile, oP = 2 * kStages * kTile, oQ = oP + 4 * kP, oCtl = oQ + 3 * kQ;
 };
 
-template <int D, int WR, int WK, int ST>
-__global__ void __launch_bounds__(32 * WR * WK, 1) attend_kernel(const Args a) {
-  using C = Cfg<D, WR, WK, ST>;
-  extern __shared__ __align__(128) uint8_t smem[];
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+template <int R>
+struct Ctl {
+  static constexpr int kMaxStages = 6;
+  uint64_t k_full[kMaxStages], k_empty[kMaxStages], v_full[kMaxStages], v_empty[kMaxStages];
+  uint64_t s_full[2], s_empty[2], p_full[2], p_empty[2], drain;
+  alignas(16) float2 rcm[R];    // row's factor from raw scores to powers of two | its reference m
+  float fac_l[R], fac_o[R];
+  float wmax[4][R], lsum[4][R];
+  float ks[kMaxStages][8], vs[kMaxStages][8];  // scales of a tile's 16-key pieces
+  int pid[kMaxStages][8];
+  uint32_t vis[R][4];           // draft of the tile sees key (bits)
+  uint32_t nan_key[kKeys][4], nan_row[R][4];
+  int low[R], top[R];           // by draft of the tile: context keys > low are seen; a chain sees keys <= top
+  int2 row[R];                  // token row, query head; -1: no row
+  uint32_t tmem;
+  volatile int abort;
+  volatile uint32_t k_it, v_it;  // tiles the loader armed (read on the abort path)
+  int nan_any;
+};
+template <int D, int R>
+size_t smem_bytes(int words, bool tree) {  // + ancestor words of the tile's drafts, parents of the sequence
+  return 1024 + Cfg<D, R>::oCtl + sizeof(Ctl<R>) + (tree ? (size_t)R * words * 4 + (size_t)words * 128 : 0);
+}
+
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+  if (ptx::mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = ptx::globaltimer_ns();
+  for (uint32_t it = 1;; ++it) {
+    if (ptx::mbar_try_wait(bar, parity)) return true;
+    if ((it & 127u) == 0) {
+      if (*abort_flag) return false;
+      if (ptx::globaltimer_ns() - t0 > kBudgetNs) {
+        *abort_flag = 1;
+        if (status) atomicExch(status, 4);
+        return false;
+      }
+    }
+  }
+}
+
+template <int D, int R>
+__global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(const Args a, const __grid_constant__ CUtensorMap tm_k,
+                                                                            const __grid_constant__ CUtensorMap tm_v) {
+  using C = Cfg<D, R>;
+  constexpr int ST = C::kStages, RH = R / 2;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  Ctl<R>& S = *reinterpret_cast<Ctl<R>*>(smem + C::oCtl);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < ST; ++i) {
+      ptx::mbar_init(&S.k_full[i], 1);
+      ptx::mbar_init(&S.k_empty[i], 1);
+      ptx::mbar_init(&S.v_full[i], 1);
+      ptx::mbar_init(&S.v_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(&S.s_full[i], 1);
+      ptx::mbar_init(&S.s_empty[i], 8);
+      ptx::mbar_init(&S.p_full[i], 8);
+      ptx::mbar_init(&S.p_empty[i], 1);
+    }
+    ptx::mbar_init(&S.drain, 1);
+    ptx::fence_mbar_init();
+    S.abort = 0;
+    S.k_it = S.v_it = 0;
+    S.nan_any = 0;
+  }
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  // Tensor memory is taken behind the wait and dependents are released behind that: no kernel holds tensor memory while
+  // it waits for one that still has to take it.
+  if (warp == 9) {
+    ptx::tmem_alloc(&S.tmem, C::kTmem);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const uint32_t tmem = S.tmem;
+
   const int page_log2 = a.c.page_log2, page = 1 << page_log2;
-  const int b = blockIdx.z, head = blockIdx.y / a.row_tiles, row0 = (blockIdx.y % a.row_tiles) * 16 * WR;
+  const int b = blockIdx.z, head = blockIdx.y / a.row_tiles, row0 = (blockIdx.y % a.row_tiles) * R;
   const Seq s = kv::sequence(a.d, b, page);
-  const int R = s.n * a.rep;
-  if (row0 >= R) return;
+  const int n_rows = s.n * a.rep;
   const int start = range_start(s, a.window);
   const int k_begin = start + blockIdx.x * a.chunk_keys;
   const int k_all = s.ctx + s.n;
-  if (k_begin >= k_all) return;
   const bool tree = a.d.parent != nullptr;
-  const int i_first = row0 / a.rep, i_last = min(R - 1, row0 + 16 * WR - 1) / a.rep;
-  int k_end = min(k_begin + a.chunk_keys, k_all);
-  if (!tree) k_end = min(k_end, s.ctx + i_last + 1);  // a chain: nobody here sees later drafts
+  const bool work = row0 < n_rows && k_begin < k_all;
+  if (work) {
+    const int i_first = row0 / a.rep, i_last = min(n_rows - 1, row0 + R - 1) / a.rep;
+    int k_end = min(k_begin + a.chunk_keys, k_all);
+    if (!tree) k_end = min(k_end, s.ctx + i_last + 1);  // a chain: nobody here sees later drafts
+    const int n_tiles = k_end > k_begin ? (k_end - k_begin + kKeys - 1) / kKeys : 0;
+    const int low_max = a.window > 0 ? s.ctx + s.n - 1 - a.window : -1;
+    const int words = tree ? (a.d.max_drafts + 31) >> 5 : 0;
 
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  const int wr = warp % WR, wk = warp / WR;
-  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + wk * (ST * C::kStage);
-  const int n_tiles = k_end > k_begin ? (k_end - k_begin + kTile - 1) / kTile : 0;
-  const int iters = (n_tiles + WK - 1) / WK;
-
-  // ---- loads: the warps of a key group bring in its tiles
-  auto load_tile = [&](int it) {
-    const int k0 = k_begin + (it * WK + wk) * kTile;
-    const uint32_t dst = ring + (it % ST) * C::kStage;
-    if (it < iters && k0 < k_end) {
-      // lane's quarter: page of keys 16 (lane & 3) .. of the tile, -1 behind the end
-      const int kq = k0 + 16 * t;
-      int pid = kq < k_all ? kv::page_of(a.d, a.c, b, kq >> page_log2) : -1;
-      const int lt = wr * 32 + lane;
-#pragma unroll
-      for (int z = 0; z < 4 * D / (32 * WR); ++z) {
-        const int p = z * 32 * WR + lt, key = p / (D / 16), c = p % (D / 16);
-        const int pg = __shfl_sync(0xffffffffu, pid, key >> 4);
-        const uint8_t* src = a.c.k + (((long long)max(pg, 0) * a.c.heads + head) << page_log2) * D + ((k0 + key) & (page - 1)) * D + c * 16;
-        const int cs = D == 128 ? c ^ (4 * (key & 1)) : c;  // odd keys swap halves: 8 lanes cover all banks
-        cp_async16(dst + key * D + cs * 16, src, pg >= 0);
+    if (warp == 8) {
+      // ------------------------------------------------------------ loader
+      asm volatile("fence.proxy.async;" ::: "memory");  // the cache was written by ordinary stores of earlier kernels
+      if (lane == 0) {
+        ptx::prefetch_tmap(&tm_k);
+        ptx::prefetch_tmap(&tm_v);
       }
-#pragma unroll
-      for (int z = 0; z < 4 * D / (32 * WR); ++z) {
-        const int p = z * 32 * WR + lt;
-        int dd, quarter;
-        if (page_log2 == 4) { dd = p % D; quarter = p / D; }
-        else if (page_log2 == 5) { dd = (p >> 1) % D; quarter = (p & 1) + 2 * ((p >> 1) / D); }
-        else { dd = p >> 2; quarter = p & 3; }
-        const int pg = __shfl_sync(0xffffffffu, pid, quarter);
-        const uint8_t* src = a.c.v + (((long long)max(pg, 0) * a.c.heads + head) << page_log2) * D + dd * page + ((k0 + 16 * quarter) & (page - 1));
-        cp_async16(dst + kTile * D + dd * kTile + quarter * 16, src, pg >= 0);
+      const int pages = kKeys >> page_log2, seg = lane & 7;
+      auto page_at = [&](int it) {
+        const int key = k_begin + it * kKeys + 16 * seg;
+        return it < n_tiles && key < k_all ? kv::page_of(a.d, a.c, b, key >> page_log2) : -1;
+      };
+      int pid = page_at(0);
+      for (int it = 0; it < n_tiles; ++it) {
+        const int st = it % ST;
+        const uint32_t parity = ((it / ST) & 1) ^ 1;
+        const int next = page_at(it + 1);
+        const int mine = __shfl_sync(0xffffffffu, pid, ((lane & 7) << page_log2) >> 4 & 7);  // page `lane` of the tile
+        const bool on = lane < pages && mine >= 0;
+        const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, on)) * page * D;
+        if (it >= ST && __any_sync(0xffffffffu, !wait(&S.k_empty[st], parity, &S.abort, a.d.status))) break;
+        uint8_t* dst = smem + C::oK + st * C::kTile + (lane & 7) * page * D;
+        if (lane == 0) {
+          ptx::mbar_arrive_expect_tx(&S.k_full[st], bytes);
+          S.k_it = it + 1;
+        }
+        __syncwarp();
+        if (on) ptx::tma_load_2d(dst, &tm_k, &S.k_full[st], 0, (mine * a.c.heads + head) << page_log2, ptx::kPolicyEvictNormal);
+        if (it >= ST && __any_sync(0xffffffffu, !wait(&S.v_empty[st], parity, &S.abort, a.d.status))) break;
+        if (lane < 8) {
+          const long long slot = (long long)max(pid, 0) * a.c.heads + head;
+          S.ks[st][lane] = pid >= 0 ? a.c.ks[slot] : 0.f;
+          S.vs[st][lane] = pid >= 0 ? a.c.vs[slot] : 0.f;
+          S.pid[st][lane] = pid;
+        }
+        __syncwarp();
+        if (lane == 0) {
+          ptx::mbar_arrive_expect_tx(&S.v_full[st], bytes);
+          S.v_it = it + 1;
+        }
+        __syncwarp();
+        dst += C::oV - C::oK;
+        if (on) {
+          if (page_log2 == 4) bulk_load(dst, a.c.v + ((long long)mine * a.c.heads + head) * (D * 16), D * 16, &S.v_full[st]);
+          else ptx::tma_load_2d(dst, &tm_v, &S.v_full[st], 0, (mine * a.c.heads + head) * D, ptx::kPolicyEvictNormal);
+        }
+        pid = next;
       }
-      if (wr == 0 && lane < 8) {
-        const long long slot = (long long)max(pid, 0) * a.c.heads + head;
-        cp_async4(dst + 2 * kTile * D + lane * 4, (lane < 4 ? a.c.ks : a.c.vs) + slot, pid >= 0);
-      }
-      if (wr == 0 && lane >= 8 && lane < 12)
-        asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst + 2 * kTile * D + lane * 4), "r"(pid) : "memory");
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
+    } else if (warp == 9) {
+      // ------------------------------------------------------------ MMA issuer
+      if (lane == 0) {
+        const uint32_t idesc = ptx::instr_desc(0, 0, R);
+        const uint32_t kb = ptx::smem_u32(smem + C::oK), vb = ptx::smem_u32(smem + C::oV), pb = ptx::smem_u32(smem + C::oP),
+                       qb = ptx::smem_u32(smem + C::oQ);
+        constexpr uint32_t kLay = D == 128 ? kSw128 : kSw64;
+        const uint32_t v_lay = page_log2 == 7 ? kSw128 : page_log2 == 6 ? kSw64 : page_log2 == 5 ? kSw32 : kSwNone;
+        const uint32_t v_str = page_log2 == 4 ? 128u : 8u << page_log2, v_lead = page_log2 == 4 ? D * 16 : 16;
+        bool ok = true;
+        auto scores = [&](int it) {
+          const int st = it % ST, u = it & 1;
+          ok = ok && wait(&S.k_full[st], (it / ST) & 1, &S.abort, a.d.status);
+          if (it >= 2) ok = ok && wait(&S.s_empty[u], ((it >> 1) & 1) ^ 1, &S.abort, a.d.status);
+          if (!ok) return;
+          ptx::tc_fence_after();
 #pragma unroll
-  for (int it = 0; it < ST - 1; ++it) load_tile(it);
-
-  // ---- ancestors of the tile's drafts, as bits over the sequence's drafts, and their depths
-  const int words = tree ? (a.d.max_drafts + 31) >> 5 : 0;
-  uint32_t* anc = reinterpret_cast<uint32_t*>(smem + C::kMain);  // [16 WR][words]
-  int* depth = reinterpret_cast<int*>(anc + 16 * WR * words);   // [16 WR]
-  int* par = depth + 16 * WR;                                   // [max_drafts]
-  if (tree) {
-    for (int i = tid; i < s.n; i += C::kThreads) par[i] = kv::parent_of(a.d.parent + s.lo, i);
-    for (int i = tid; i < 16 * WR * words; i += C::kThreads) anc[i] = 0;
-    __syncthreads();
-    for (int l = tid; l <= i_last - i_first; l += C::kThreads) {
-      int n = 0;
-      for (int j = i_first + l; j >= 0; j = par[j], ++n)  // parents come earlier: at most s.n steps
-        if (a.window <= 0 || n < a.window) anc[l * words + (j >> 5)] |= 1u << (j & 31);
-      depth[l] = n - 1;
-    }
-    __syncthreads();
-  }
-
-  // ---- this lane's rows: g and g + 8 of the warp's 16
-  uint32_t qf[D / 16][4];
-  float rc[2];              // row's factor from raw scores to powers of two
-  int low[2], top[2], loc[2];  // context keys > low are seen; a chain sees keys <= top
-  bool live[2];
+          for (int term = 0; term < 3; ++term)
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r = row0 + wr * 16 + g + 8 * h;
-    live[h] = r < R;
-    const int rr = live[h] ? r : R - 1, i = rr / a.rep, hq = head * a.rep + rr % a.rep;
-    const __nv_bfloat16* src = a.q + (long long)(s.lo + i) * a.q_stride + (long long)hq * D;
-    float v[D / 64][16];
-    float m = 0.f;
+            for (int k = 0; k < D / 32; ++k)
+              ptx::mma_f8f6f4(tmem + u * R, desc_of(kb + st * C::kTile + k * 32, 16, 8 * D, kLay),
+                              desc_of(qb + term * C::kQ + k * 32, 16, 8 * D, kLay), idesc, term + k > 0);
+          ptx::mma_commit(&S.k_empty[st]);
+          ptx::mma_commit(&S.s_full[u]);
+        };
+        if (n_tiles > 0) {
+          ok = wait(&S.drain, 0, &S.abort, a.d.status);  // Q is there
+          scores(0);
+        }
+        for (int it = 0; it < n_tiles && ok; ++it) {
+          if (it + 1 < n_tiles) scores(it + 1);
+          const int st = it % ST, u = it & 1;
+          ok = ok && wait(&S.v_full[st], (it / ST) & 1, &S.abort, a.d.status);
+          ok = ok && wait(&S.p_full[u], (it >> 1) & 1, &S.abort, a.d.status);
+          if (!ok) break;
+          ptx::tc_fence_after();
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-      float x[8], y[8];
-      kv::load8(src + (t + 4 * c) * 16, x);
-      kv::load8(src + (t + 4 * c) * 16 + 8, y);
+          for (int term = 0; term < 2; ++term)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { v[c][e] = x[e]; v[c][8 + e] = y[e]; m = fmaxf(m, fmaxf(fabsf(x[e]), fabsf(y[e]))); }
-    }
-    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-    // 2^e in [m, 2 m), brought to 2^14; a zero, infinite or NaN row as it is
-    const uint32_t e = __float_as_uint(m) >> 23;
-    float up = 1.f, back = 1.f;
-    if (e >= 30u && e < 255u) {
-      const int x = 13 - ((int)e - 127);  // largest element to [2^13, 2^14)
-      up = ldexpf(1.f, x);
-      back = ldexpf(1.f, -x);
-    }
-    rc[h] = a.scale_log2 * back;
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        qf[4 * c + w][h] = pack_f16(v[c][4 * w] * up, v[c][4 * w + 1] * up);
-        qf[4 * c + w][2 + h] = pack_f16(v[c][4 * w + 2] * up, v[c][4 * w + 3] * up);
-      }
-    loc[h] = i - i_first;
-    const int at = s.ctx + (tree ? depth[loc[h]] : i);
-    low[h] = a.window > 0 ? at - a.window : -1;
-    top[h] = tree ? s.ctx - 1 : at;  // last key of the contiguous part
-  }
-  const int low_max = a.window > 0 ? s.ctx + s.n - 1 - a.window : -1;  // no row hides a key above this
-
-  float o[D / 8][4] = {};
-  float mx[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-  float u = 1.17549435e-38f;
-
-  for (int it = 0; it < iters; ++it) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(ST - 2) : "memory");
-    if constexpr (WR == 1) __syncwarp();
-    else asm volatile("bar.sync %0, %1;" ::"r"(1 + wk), "r"(32 * WR) : "memory");
-    load_tile(it + ST - 1);
-    const int k0 = k_begin + (it * WK + wk) * kTile;
-    if (k0 >= k_end) continue;
-    const uint32_t ks = ring + (it % ST) * C::kStage, vs = ks + kTile * D;
-    float sc[8][4] = {};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t row = ks + (16 * (g >> 1) + 2 * j + (g & 1)) * D;
-#pragma unroll
-      for (int c = 0; c < D / 64; ++c) {
-        const uint4 w = lds128(row + (((t + 4 * c) ^ (D == 128 ? 4 * (g & 1) : 0)) * 16));
-        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          uint32_t b0, b1;
-          codes_to_f16(ww[e], b0, b1);
-          mma_f16(sc[j], qf[4 * c + e], b0, b1);
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t step = page_log2 == 7 ? k * 32 : page_log2 == 6 ? (k >> 1) * (D * 64) + (k & 1) * 32 : k * (D * 32);
+              ptx::mma_f8f6f4(tmem + (2 + term) * R, desc_of(vb + st * C::kTile + step, v_lead, v_str, v_lay),
+                              desc_of(pb + (2 * u + term) * C::kP + k * 32, 16, 1024, kSw128), idesc, it + k > 0);
+            }
+          ptx::mma_commit(&S.v_empty[st]);
+          ptx::mma_commit(&S.p_empty[u]);
+        }
+        if (!ok) {  // abort: what was issued must have ended before tensor memory and shared memory are given back
+          ptx::mma_commit(&S.drain);
+          ptx::drain_wait(&S.drain, 1, kBudgetNs);
         }
       }
-    }
-    float k_scale, v_scale;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k_scale) : "r"(vs + kTile * D + 4 * t));
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v_scale) : "r"(vs + kTile * D + 16 + 4 * t));
-    // lane t's keys: k0 + 16 t + 2 j + e
-    const int kq = k0 + 16 * t;
-    const bool masked = k0 + kTile > s.ctx || k0 <= low_max;
-    uint32_t see[2] = {0xffffu, 0xffffu};
-    int pid;  // -1: behind the end, or a page id outside the pool; its keys are not seen
-    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(pid) : "r"(vs + kTile * D + 32 + 4 * t));
-    if (pid < 0) see[0] = see[1] = 0;
-    if (masked) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        // keys low + 1 .. top
-        const int from = max(0, low[h] + 1 - kq), to = min(16, top[h] + 1 - kq);
-        uint32_t bits = to > from ? (0xffffu >> (16 - to)) & (0xffffu << from) : 0u;
-        if (tree && kq + 16 > s.ctx && kq < k_all) {
-          const int off = kq - s.ctx;  // draft index of the lane's first key, may be negative
-          uint64_t w;
-          const uint32_t* an = anc + loc[h] * words;
-          if (off < 0) w = (uint64_t)an[0] << (-off);
-          else {
-            const int wi = off >> 5;
-            w = ((uint64_t)an[wi] | (wi + 1 < words ? (uint64_t)an[wi + 1] << 32 : 0ull)) >> (off & 31);
-          }
-          bits |= (uint32_t)w & 0xffffu;
-        }
-        see[h] &= bits;
-      }
-    }
-    float mt[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int h = e >> 1;
-        float v = sc[j][e] * k_scale;
-        v = (see[h] >> (2 * j + (e & 1))) & 1u ? v : -INFINITY;
-        sc[j][e] = v;
-        mt[h] = fmaxf(mt[h], v);
-      }
-    float vm = v_scale;
-    vm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, 1));
-    vm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, 2));
-    const float u_new = fmaxf(u, vm), ur = u / u_new;
-    float alpha[2], mr[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      mt[h] = fmaxf(mt[h], __shfl_xor_sync(0xffffffffu, mt[h], 1));
-      mt[h] = fmaxf(mt[h], __shfl_xor_sync(0xffffffffu, mt[h], 2));
-      const float m_new = fmaxf(mx[h], mt[h]);
-      const float m_ref = m_new == -INFINITY ? 0.f : m_new;
-      alpha[h] = exp2_fast((mx[h] - m_ref) * rc[h]);
-      mr[h] = m_ref * rc[h];
-      mx[h] = m_new;
-      l[h] *= alpha[h];
-      alpha[h] *= ur;
-    }
-    u = u_new;
-    const float f = v_scale / u * 16384.f;
-    uint32_t pf[4][4];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float p[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        p[e] = exp2_fast(fmaf(sc[j][e], rc[e >> 1], -mr[e >> 1]));
-        l[e >> 1] += p[e];
-        p[e] *= f;
-      }
-      pf[j >> 1][2 * (j & 1)] = pack_f16(p[0], p[1]);
-      pf[j >> 1][2 * (j & 1) + 1] = pack_f16(p[2], p[3]);
-    }
-    if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
-#pragma unroll
-      for (int d = 0; d < D / 8; ++d) {
-        o[d][0] *= alpha[0];
-        o[d][1] *= alpha[0];
-        o[d][2] *= alpha[1];
-        o[d][3] *= alpha[1];
-      }
-    }
-    uint32_t nan_codes = 0;
-#pragma unroll
-    for (int d = 0; d < D / 8; ++d) {
-      const uint4 w = lds128(vs + (8 * d + g) * kTile + t * 16);
-      uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-      if (masked) {  // a NaN code must not reach rows that do not see its key: 0 * NaN
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t bad = __vcmpeq4(ww[e] & 0x7f7f7f7fu, 0x7f7f7f7fu);
-          nan_codes |= bad;
-          ww[e] &= ~bad;
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        uint32_t b0, b1;
-        codes_to_f16(ww[e], b0, b1);
-        mma_f16(o[d], pf[e], b0, b1);
-      }
-    }
-    if (masked && __any_sync(0xffffffffu, nan_codes != 0)) {
-      // rows that do see one: their output is NaN in that dimension (ones in the place of the NaN codes)
-#pragma unroll 1
-      for (int d = 0; d < D / 8; ++d) {
-        const uint4 w = lds128(vs + (8 * d + g) * kTile + t * 16);
-        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-        float hit[4] = {};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          uint32_t b0, b1;
-          codes_to_f16(__vcmpeq4(ww[e] & 0x7f7f7f7fu, 0x7f7f7f7fu) & 0x38383838u, b0, b1);
-          mma_f16(hit, pf[e], b0, b1);
-        }
-#pragma unroll
-        for (int dd = 0; dd < D / 8; ++dd)
-          if (dd == d)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (hit[e] > 0.f) o[dd][e] = __int_as_float(0x7fffffff);
-      }
-    }
-  }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-    mx[h] *= rc[h];  // to powers of two
-  }
-  const float back = u * (1.f / 16384.f);
-#pragma unroll
-  for (int d = 0; d < D / 8; ++d)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[d][e] *= back;
-
-  // one row's result: unnormalised o[c], c = 8 d + 2 t + e
-  const bool split = a.chunks > 1;
-  auto write2 = [&](int r, int c, float x, float y, float m, float den) {
-    const int i = r / a.rep, hq = head * a.rep + r % a.rep;
-    const long long token = s.lo + i;
-    if (split) {
-      const long long at = ((long long)blockIdx.x * a.d.n_tokens + token) * a.n_heads + hq;
-      *reinterpret_cast<float2*>(a.part_o + at * D + c) = make_float2(x, y);
-      if (c == 0) a.part_ml[at] = make_float2(m, den);
     } else {
-      if (a.sinks) {
-        const float sk = a.sinks[hq] * 1.4426950408889634f, mm = fmaxf(m, sk);
-        const float w = exp2_fast(m - mm);
-        den = den * w + exp2_fast(sk - mm);
-        x *= w;
-        y *= w;
-        m = mm;
+      // ------------------------------------------------------------ softmax
+      const int quad = warp & 3, half = warp >> 2, r0 = half * RH, key = quad * 32 + lane;
+      uint32_t* anc = reinterpret_cast<uint32_t*>(smem + C::oCtl + sizeof(Ctl<R>));  // [R][words]
+      int* par = reinterpret_cast<int*>(anc + R * words);
+      if (tree) {
+        for (int i = tid; i < s.n; i += 256) par[i] = kv::parent_of(a.d.parent + s.lo, i);
+        for (int i = tid; i < R * words; i += 256) anc[i] = 0;
+        ptx::named_barrier(2, 256);
       }
-      const float inv = den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den);
-      const __nv_bfloat162 v = __floats2bfloat162_rn(x * inv, y * inv);
-      *reinterpret_cast<__nv_bfloat162*>(a.out + token * a.out_stride + (long long)hq * D + c) = v;
-      if (c == 0 && a.lse) a.lse[token * a.n_heads + hq] = den == 0.f ? -INFINITY : (m + log2f(den)) * 0.6931471805599453f;
+      if (tid <= i_last - i_first) {  // one thread per draft of the tile
+        const int i = i_first + tid;
+        int at = s.ctx + i;
+        if (tree) {
+          int n = 0;
+          for (int j = i; j >= 0; j = par[j], ++n)  // parents come earlier: at most s.n steps
+            if (a.window <= 0 || n < a.window) anc[tid * words + (j >> 5)] |= 1u << (j & 31);
+          at = s.ctx + n - 1;
+        }
+        S.low[tid] = a.window > 0 ? at - a.window : -1;
+        S.top[tid] = tree ? s.ctx - 1 : at;
+      }
+      for (int i = tid; i < R * 4; i += 256) (&S.nan_row[0][0])[i] = 0;
+      // Q: a row's D elements by D / 8 neighbouring lanes, 8 each
+      constexpr int kPer = D / 8;
+      for (int z = tid; z < R * kPer; z += 256) {
+        const int r = z / kPer, d0 = (z % kPer) * 8, rr = row0 + r;
+        const bool live = rr < n_rows;
+        const int i = rr / a.rep, hq = head * a.rep + rr % a.rep;
+        float v[8] = {};
+        if (live) kv::load8(a.q + (long long)(s.lo + i) * a.q_stride + (long long)hq * D + d0, v);
+        float m = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e]));
+        const uint32_t lanes = D == 128 ? 0xffffu << (lane & 16) : 0xffu << (lane & 24);
+#pragma unroll
+        for (int o = kPer / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(lanes, m, o));
+        // 2^e <= m < 2^(e + 1), brought to [128, 256); a zero, infinite or NaN row as it is
+        const int ex = (int)(__float_as_uint(m) >> 23) - 127;
+        float up = 1.f, back = 1.f;
+        if (ex >= -110 && ex < 128) {
+          up = ldexpf(1.f, 7 - ex);
+          back = ldexpf(1.f, ex - 7);
+        }
+        if ((z % kPer) == 0) {
+          S.rcm[r] = make_float2(a.scale_log2 * back, kUnseen);
+          S.row[r] = live ? make_int2(s.lo + i, hq) : make_int2(-1, 0);
+        }
+        uint32_t code[3][2] = {};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float x = v[e] * up;
+#pragma unroll
+          for (int term = 0; term < 3; ++term) {
+            // infinities become NaN: a row with one has NaN scores, as inf * 0 and inf - inf have it
+            const __nv_fp8_storage_t c = fabsf(x) <= 448.f ? __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3) : (__nv_fp8_storage_t)0x7F;
+            const __half_raw h = __nv_cvt_fp8_to_halfraw(c, __NV_E4M3);
+            x -= __half2float(*reinterpret_cast<const __half*>(&h));
+            code[term][e >> 2] |= (uint32_t)c << (8 * (e & 3));
+          }
+        }
+#pragma unroll
+        for (int term = 0; term < 3; ++term)
+          *reinterpret_cast<uint2*>(smem + C::oQ + term * C::kQ + q_byte<D>(r, d0)) = make_uint2(code[term][0], code[term][1]);
+      }
+      ptx::fence_proxy_async_smem();
+      ptx::named_barrier(2, 256);
+      if (tid == 0) ptx::mbar_arrive(&S.drain);
+
+      float l[RH];
+#pragma unroll
+      for (int r = 0; r < RH; ++r) l[r] = 0.f;
+      float u = 0.f;  // V scale that the accumulators are in units of
+      const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
+      uint32_t xo[8];  // this key's byte in row r of P: (r & 7) selects
+#pragma unroll
+      for (int k = 0; k < 8; ++k) xo[k] = (((key >> 4) ^ k) << 4) + (key & 15);
+      bool ok = true;
+      for (int it = 0; it < n_tiles; ++it) {
+        const int st = it % ST, bu = it & 1;
+        const int k0 = k_begin + it * kKeys;
+        ok = wait(&S.v_full[st], (it / ST) & 1, &S.abort, a.d.status) && ok;
+        // a thread that gave up stays with the others' barriers until here, where all of them leave
+        if (any_of_256(!ok)) {
+          ok = false;
+          break;
+        }
+        bool masked = k0 + kKeys > s.ctx || k0 <= low_max;  // somebody may not see a key of the tile
+#pragma unroll
+        for (int e = 0; e < 8; ++e) masked = masked || S.pid[st][e] < 0;
+        if (masked) {
+          // what each draft of the tile sees of its keys
+          for (int z = tid; z < (i_last - i_first + 1) * 4; z += 256) {
+            const int dr = z >> 2, kb = k0 + (z & 3) * 32;
+            const int from = max(0, S.low[dr] + 1 - kb), to = min(32, S.top[dr] + 1 - kb);
+            uint32_t bits = to > from ? (0xffffffffu >> (32 - to)) & (0xffffffffu << from) : 0u;
+            if (tree && kb + 32 > s.ctx && kb < k_all) {
+              const int off = kb - s.ctx;  // draft of the word's first key, may be negative
+              const uint32_t* an = anc + dr * words;
+              if (off < 0) bits |= an[0] << -off;
+              else bits |= __funnelshift_r(an[off >> 5], (off >> 5) + 1 < words ? an[(off >> 5) + 1] : 0u, off & 31);
+            }
+            // pages that are not there
+            if (S.pid[st][2 * (z & 3)] < 0) bits &= 0xffff0000u;
+            if (S.pid[st][2 * (z & 3) + 1] < 0) bits &= 0x0000ffffu;
+            S.vis[dr][z & 3] = bits;
+          }
+          for (int z = tid; z < kKeys * 4; z += 256) (&S.nan_key[0][0])[z] = 0;
+          if (tid == 0) S.nan_any = 0;
+          ptx::named_barrier(2, 256);
+          // V of keys behind the end or without a page becomes zero, so that 0 * V is 0; a NaN of a written key is taken out
+          // too and kept as bits, for the rows that do see the key
+          uint8_t* vt = smem + C::oV + st * C::kTile;
+          for (int z = tid; z < D * 8; z += 256) {
+            const int d = z >> 3, seg = z & 7;
+            const int have = S.pid[st][seg] < 0 ? 0 : min(16, max(0, k_all - (k0 + 16 * seg)));
+            uint4* at = reinterpret_cast<uint4*>(vt + v_piece<D>(d, seg, page_log2));
+            uint4 w = have > 0 ? *at : make_uint4(0, 0, 0, 0);
+            uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+            bool changed = have < 16;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int keep = min(4, max(0, have - 4 * e));
+              if (keep < 4) ww[e] &= keep == 0 ? 0u : 0xffffffffu >> (32 - 8 * keep);
+              uint32_t bad = __vcmpeq4(ww[e] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+              if (bad) {
+                ww[e] &= ~bad;
+                changed = true;
+                S.nan_any = 1;
+                for (int y = 0; y < 4; ++y)
+                  if ((bad >> (8 * y)) & 1u) atomicOr(&S.nan_key[seg * 16 + 4 * e + y][d >> 5], 1u << (d & 31));
+              }
+            }
+            if (changed) *at = make_uint4(ww[0], ww[1], ww[2], ww[3]);
+          }
+          ptx::named_barrier(2, 256);
+          if (S.nan_any) {
+            uint32_t nk[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) nk[y] = S.nan_key[key][y];
+            if (nk[0] | nk[1] | nk[2] | nk[3])
+              for (int r = r0; r < r0 + RH; ++r)
+                if (row0 + r < n_rows && (S.vis[(row0 + r) / a.rep - i_first][key >> 5] >> (key & 31)) & 1u)
+                  for (int y = 0; y < 4; ++y)
+                    if (nk[y]) atomicOr(&S.nan_row[r][y], nk[y]);
+          }
+        }
+        ok = wait(&S.s_full[bu], (it >> 1) & 1, &S.abort, a.d.status) && ok;
+        ptx::tc_fence_after();
+        float v[RH];
+#pragma unroll
+        for (int c = 0; c < RH / 8; ++c) tmem_ld8(tmem + lane_base + bu * R + r0 + 8 * c, *reinterpret_cast<uint32_t(*)[8]>(&v[8 * c]));
+        ptx::tmem_ld_wait();
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&S.s_empty[bu]);
+
+        const float k_scale = S.ks[st][key >> 4], v_scale = S.vs[st][key >> 4];
+        float vm = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vm = fmaxf(vm, S.vs[st][e]);
+        const bool unit = vm > u || vm < u * (1.f / 64.f);  // the same in every thread
+#pragma unroll
+        for (int r = 0; r < RH; ++r) v[r] *= k_scale;
+        if (masked) {
+#pragma unroll
+          for (int r = 0; r < RH; ++r) {
+            const int rr = min(row0 + r0 + r, n_rows - 1);
+            if (!((S.vis[rr / a.rep - i_first][quad] >> lane) & 1u)) v[r] = -INFINITY;
+          }
+        }
+        float tmax = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < RH; ++r) {
+          const float2 q = S.rcm[r0 + r];
+          tmax = fmaxf(tmax, fmaf(v[r], q.x, -q.y));
+        }
+        if (any_of_256(tmax > kLimit || (unit && vm > 0.f))) {
+          // move the references to the maxima and the unit to the tile's largest V scale
+#pragma unroll
+          for (int r = 0; r < RH; ++r) {
+            const float m = warp_max(v[r] * S.rcm[r0 + r].x);
+            if (lane == 0) S.wmax[quad][r0 + r] = m;
+          }
+          ptx::named_barrier(2, 256);
+          const float u_new = unit && vm > 0.f ? vm : u;
+          if (tid < R) {
+            const float old = S.rcm[tid].y;
+            const float m = fmaxf(fmaxf(old, fmaxf(S.wmax[0][tid], S.wmax[1][tid])), fmaxf(S.wmax[2][tid], S.wmax[3][tid]));
+            const float fl = exp2_fast(old - m);
+            S.rcm[tid].y = m;
+            S.fac_l[tid] = fl;
+            S.fac_o[tid] = fl * (u / u_new);
+          }
+          ptx::named_barrier(2, 256);
+          u = u_new;
+#pragma unroll
+          for (int r = 0; r < RH; ++r) l[r] *= S.fac_l[r0 + r];
+          if (it > 0) {
+            ok = wait(&S.p_empty[bu ^ 1], ((it - 1) >> 1) & 1, &S.abort, a.d.status) && ok;  // the product of tile it - 1 has ended
+            ptx::tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < RH / 8; ++c)
+#pragma unroll
+              for (int term = 0; term < 2; ++term) {
+                uint32_t o[8];
+                const uint32_t at = tmem + lane_base + (2 + term) * R + r0 + 8 * c;
+                tmem_ld8(at, o);
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * S.fac_o[r0 + 8 * c + e]);
+                tmem_st8(at, o);
+              }
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            ptx::tc_fence_before();
+          }
+        }
+        if (it >= 2) ok = wait(&S.p_empty[bu], ((it >> 1) & 1) ^ 1, &S.abort, a.d.status) && ok;
+        const float f = u > 0.f ? v_scale / u * kUp : 0.f;
+        uint8_t* ph = smem + C::oP + (2 * bu) * C::kP + r0 * 128;
+#pragma unroll
+        for (int r = 0; r < RH; r += 2) {
+          const float4 q = *reinterpret_cast<const float4*>(&S.rcm[r0 + r]);
+          const float p0 = exp2_fast(fmaf(v[r], q.x, -q.y)), p1 = exp2_fast(fmaf(v[r + 1], q.z, -q.w));
+          l[r] += p0;
+          l[r + 1] += p1;
+          const __half2 h = __floats2half2_rn(p0 * f, p1 * f);
+          const uint32_t hi = f16_to_codes(*reinterpret_cast<const uint32_t*>(&h));
+          const uint32_t bk = codes_to_f16(hi);
+          const __half2 rest = __hmul2(__hsub2(h, *reinterpret_cast<const __half2*>(&bk)), __half2half2(__ushort_as_half(0x4C00)));  // * 16
+          const uint32_t lo = f16_to_codes(*reinterpret_cast<const uint32_t*>(&rest));
+          ph[r * 128 + xo[r & 7]] = (uint8_t)hi;
+          ph[(r + 1) * 128 + xo[(r + 1) & 7]] = (uint8_t)(hi >> 8);
+          ph[C::kP + r * 128 + xo[r & 7]] = (uint8_t)lo;
+          ph[C::kP + (r + 1) * 128 + xo[(r + 1) & 7]] = (uint8_t)(lo >> 8);
+        }
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&S.p_full[bu]);
+      }
+      // ---- results
+      if (ok && n_tiles > 0) ok = wait(&S.p_empty[(n_tiles - 1) & 1], ((n_tiles - 1) >> 1) & 1, &S.abort, a.d.status);
+      ptx::tc_fence_after();
+#pragma unroll
+      for (int r = 0; r < RH; ++r) {
+        float x = l[r];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        if (lane == 0) S.lsum[quad][r0 + r] = x;
+      }
+      if (!any_of_256(!ok)) {
+        const float back = u * kDown;
+        const int d = quad * 32 + lane;
+        const bool split = a.chunks > 1;
+#pragma unroll 1
+        for (int c = 0; c < RH / 8; ++c) {
+          uint32_t oh[8], ol[8];
+          const uint32_t at = tmem + lane_base + 2 * R + r0 + 8 * c;
+          if (n_tiles > 0) {
+            tmem_ld8(at, oh);
+            tmem_ld8(at + R, ol);
+            ptx::tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) oh[e] = ol[e] = 0u;
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int r = r0 + 8 * c + e;
+            const int2 ro = S.row[r];
+            if (ro.x < 0 || d >= D) continue;
+            float den = (S.lsum[0][r] + S.lsum[1][r]) + (S.lsum[2][r] + S.lsum[3][r]);
+            float m = den == 0.f ? -INFINITY : S.rcm[r].y;
+            float o = (__uint_as_float(oh[e]) + 0.0625f * __uint_as_float(ol[e])) * back;
+            if ((S.nan_row[r][d >> 5] >> (d & 31)) & 1u) o = __int_as_float(0x7fffffff);
+            if (split) {
+              const long long w = ((long long)blockIdx.x * a.d.n_tokens + ro.x) * a.n_heads + ro.y;
+              a.part_o[w * D + d] = o;
+              if (d == 0) a.part_ml[w] = make_float2(m, den);
+            } else {
+              if (a.sinks) {
+                const float sk = a.sinks[ro.y] * 1.4426950408889634f, mm = fmaxf(m, sk), g = exp2_fast(m - mm);
+                den = den * g + exp2_fast(sk - mm);
+                o *= g;
+                m = mm;
+              }
+              const float inv = den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den);
+              a.out[(long long)ro.x * a.out_stride + (long long)ro.y * D + d] = __float2bfloat16_rn(o * inv);
+              if (d == 0 && a.lse) a.lse[(long long)ro.x * a.n_heads + ro.y] = den == 0.f ? -INFINITY : (m + log2f(den)) * 0.6931471805599453f;
+            }
+          }
+        }
+      }
     }
-  };
-  if constexpr (WK == 1) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (live[h]) {
-#pragma unroll
-        for (int d = 0; d < D / 8; ++d)
-          write2(row0 + wr * 16 + g + 8 * h, 8 * d + 2 * t, o[d][2 * h], o[d][2 * h + 1], mx[h], l[h]);
-      }
-  } else {
-    constexpr int P = D + 4;
-    float* om = reinterpret_cast<float*>(smem);       // [WK][16 WR][P]
-    float* ml = om + WK * 16 * WR * P;                // [WK][16 WR][2]
-    __syncthreads();  // all tiles are used up
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int r = wk * 16 * WR + wr * 16 + g + 8 * h;
-#pragma unroll
-      for (int d = 0; d < D / 8; ++d) *reinterpret_cast<float2*>(om + r * P + 8 * d + 2 * t) = make_float2(o[d][2 * h], o[d][2 * h + 1]);
-      if (t == 0) { ml[2 * r] = mx[h]; ml[2 * r + 1] = l[h]; }
-    }
-    __syncthreads();
-    for (int z = tid; z < 16 * WR * (D / 2); z += C::kThreads) {
-      const int r = z / (D / 2), c = (z % (D / 2)) * 2;
-      if (row0 + r >= R) continue;
-      float m = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < WK; ++k) m = fmaxf(m, ml[2 * (k * 16 * WR + r)]);
-      const float mr = m == -INFINITY ? 0.f : m;
-      float den = 0.f, x = 0.f, y = 0.f;
-#pragma unroll
-      for (int k = 0; k < WK; ++k) {
-        const int q = k * 16 * WR + r;
-        const float w = exp2_fast(ml[2 * q] - mr);
-        const float2 v = *reinterpret_cast<const float2*>(om + q * P + c);
-        den = fmaf(w, ml[2 * q + 1], den);
-        x = fmaf(w, v.x, x);
-        y = fmaf(w, v.y, y);
-      }
-      write2(row0 + r, c, x, y, m, den);
+    if (S.abort && warp == 8 && lane == 0) {  // copies in flight land before the shared memory is given back
+      ptx::drain_ring(S.k_full, ST, S.k_it, kBudgetNs);
+      ptx::drain_ring(S.v_full, ST, S.v_it, kBudgetNs);
     }
   }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  if (warp == 9) ptx::tmem_dealloc(tmem, C::kTmem);
 }
 
 // One warp per (token, head): the chunks' parts, in order, and the sink.

@@ -138,6 +138,8 @@ bool batch_ok(const moev_kv_cache* c, const moev_draft_batch* d) {
     return false;
   if (d->n_seq < 0 || d->n_seq > 65535 || d->n_tokens < 0 || d->max_drafts < 1 || d->max_len < d->max_drafts || d->table_cols < 1) return false;
   if (d->max_len > (1 << 30) || d->max_drafts > (1 << 24)) return false;
+  // coordinates of the rows of K and V are 32 bits wide
+  if ((long long)c->n_pages * c->n_kv_heads * std::max(c->page, c->head_dim) > 0x7fffffffLL) return false;
   if (d->parent && d->max_drafts > kv::kMaxTree) return false;
   return d->cu && d->ctx_len && d->page_table;
 }
@@ -151,50 +153,76 @@ kv::Cache cache_of(const moev_kv_cache* c) {
 }
 
 struct Plan {
-  int wr, wk, row_tiles, chunks, chunk_keys;
+  int rows, row_tiles, chunks, chunk_keys;  // rows of a tile
 };
 Plan attend_plan(const moev_kv_cache* c, const moev_draft_batch* d, int n_heads, int window) {
   Plan p;
   const int rep = n_heads / c->n_kv_heads;
   const long long rows = (long long)d->max_drafts * rep;
-  if (rows <= 16) { p.wr = 1; p.wk = 4; }
-  else if (rows <= 32) { p.wr = 2; p.wk = 4; }
-  else if (rows <= 64) { p.wr = 4; p.wk = 2; }
-  else { p.wr = 8; p.wk = 1; }
-  p.row_tiles = (int)((rows + 16 * p.wr - 1) / (16 * p.wr));
+  p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  // a tile of 128 rows and the ancestors of very large trees do not fit together
+  if (p.rows == 128 && att::smem_bytes<128, 128>((d->max_drafts + 31) / 32, d->parent != nullptr) > 227 * 1024) p.rows = 64;
+  p.row_tiles = (int)((rows + p.rows - 1) / p.rows);
   long long span = d->max_len;
-  if (window > 0) span = std::min<long long>(span, (long long)window + d->max_drafts + 63);
+  if (window > 0) span = std::min<long long>(span, (long long)window + d->max_drafts + att::kKeys - 1);
   const long long base = (long long)std::max(1, d->n_seq) * c->n_kv_heads * p.row_tiles;
-  const int sms = sm_count();
+  const int slots = sm_count() * (p.rows <= 32 ? 2 : 1);
   // one wave of CTAs while that splits the keys at all; with many sequences or heads several waves, whose
   // chunks even out their different lengths, but no chunk below 1024 keys
-  const int unit = 64 * p.wk;
-  long long want, least = unit;
-  if (base * 2 <= sms) want = sms / base;
+  long long want, least = att::kKeys;
+  if (base * 2 <= slots) want = slots / base;
   else {
-    want = (8LL * sms + base - 1) / base;
+    want = (4LL * slots + base - 1) / base;
     least = 1024;
   }
   long long keys = std::max<long long>((span + want - 1) / want, least);
-  keys = (keys + unit - 1) / unit * unit;
+  keys = (keys + att::kKeys - 1) / att::kKeys * att::kKeys;
   p.chunk_keys = (int)keys;
   p.chunks = (int)((span + keys - 1) / keys);
   return p;
 }
 
-template <int D, int WR, int WK, int ST>
-cudaError_t launch_attend(const att::Args& a, cudaStream_t st) {
-  const int words = (a.d.max_drafts + 31) / 32;
-  const size_t smem = att::Cfg<D, WR, WK, ST>::smem(words, a.d.parent != nullptr);
-  return launch(att::attend_kernel<D, WR, WK, ST>, dim3(a.chunks, a.c.heads * a.row_tiles, a.d.n_seq), dim3(32 * WR * WK), smem, st, a);
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn() {
+  static EncodeTiledFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const bool ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess;
+    return ok ? reinterpret_cast<EncodeTiledFn>(p) : nullptr;
+  }();
+  return fn;
+}
+// rows of `width` bytes (16 to 128), `box` of them at a time, in the swizzle of that width
+bool encode_rows(CUtensorMap* m, const void* ptr, int width, long long rows, int box) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)width};
+  const cuuint32_t b[2] = {(cuuint32_t)width, (cuuint32_t)box}, es[2] = {1, 1};
+  const CUtensorMapSwizzle sw = width == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
+                                : width == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                : width == 32 ? CU_TENSOR_MAP_SWIZZLE_32B
+                                              : CU_TENSOR_MAP_SWIZZLE_NONE;
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, b, es, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int R>
+cudaError_t launch_attend(const att::Args& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
+  const size_t smem = att::smem_bytes<D, R>((a.d.max_drafts + 31) / 32, a.d.parent != nullptr);
+  return launch(att::attend_kernel<D, R>, dim3(a.chunks, a.c.heads * a.row_tiles, a.d.n_seq), dim3(att::kThreads), smem, st, a, tk, tv);
 }
 template <int D>
-cudaError_t launch_attend_d(const att::Args& a, int wr, cudaStream_t st) {
+cudaError_t launch_attend_d(const att::Args& a, int rows, cudaStream_t st) {
+  const int page = 1 << a.c.page_log2;
+  const long long blocks = (long long)a.c.n_pages * a.c.heads;
+  CUtensorMap tk, tv;
+  if (!encode_rows(&tk, a.c.k, D, blocks * page, page) || !encode_rows(&tv, a.c.v, page, blocks * D, D)) return cudaErrorUnknown;
   cudaError_t e;
-  if (wr == 1) e = launch_attend<D, 1, 4, 3>(a, st);
-  else if (wr == 2) e = launch_attend<D, 2, 4, 3>(a, st);
-  else if (wr == 4) e = launch_attend<D, 4, 2, 4>(a, st);
-  else e = launch_attend<D, 8, 1, 3>(a, st);
+  if (rows == 16) e = launch_attend<D, 16>(a, tk, tv, st);
+  else if (rows == 32) e = launch_attend<D, 32>(a, tk, tv, st);
+  else if (rows == 64) e = launch_attend<D, 64>(a, tk, tv, st);
+  else e = launch_attend<D, 128>(a, tk, tv, st);
   if (e != cudaSuccess || a.chunks == 1) return e;
   return launch(att::attend_combine_kernel<D>, dim3(a.d.max_drafts, (a.n_heads + 3) / 4, a.d.n_seq), dim3(128), 0, st, a);
 }
@@ -355,7 +383,7 @@ moev_status moev_cache_attend(const moev_kv_cache* c, const moev_draft_batch* d,
   a.window = window;
   a.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  return done(c->head_dim == 64 ? launch_attend_d<64>(a, p.wr, st) : launch_attend_d<128>(a, p.wr, st));
+  return done(c->head_dim == 64 ? launch_attend_d<64>(a, p.rows, st) : launch_attend_d<128>(a, p.rows, st));
 }
 
 }  // extern "C"

@@ -106,17 +106,18 @@ class Setup:
         return self.ctx[b] + len(ancestors(self.parents[b])[i]) - 1
 
     def attend(self, window=0, sinks=None, scale=None):
-        """(out, lse, sum of p |v|, bound of the scores' binary32 error), rows of no sequence as zeros."""
+        """(out, lse, sum of p |v|, bound of the scores' error, floor of the probabilities' error), rows of no sequence as zeros."""
         D, page, rep = self.D, self.page, self.rep
         scale = D ** -0.5 if scale is None else scale
         out = torch.zeros(self.T, self.heads * rep, D, dtype=torch.float64)
         lse, mass = torch.zeros(self.T, self.heads * rep, dtype=torch.float64), torch.zeros_like(out)
-        ds = torch.zeros_like(lse)
+        ds, floor = torch.zeros_like(lse), torch.zeros_like(out)
         for b, (c, n) in enumerate(zip(self.ctx, self.cnt)):
             if not n:
                 continue
             pages = self.table[b, :-(-(c + n) // page)].long()
             k = (self.k[pages].double() * self.ks[pages].double()[..., None, None]).permute(1, 0, 2, 3).reshape(self.heads, -1, D)
+            code = self.v[pages].double().permute(1, 0, 3, 2).reshape(self.heads, -1, D)
             v = (self.v[pages].double() * self.vs[pages].double()[..., None, None]).permute(1, 0, 3, 2).reshape(self.heads, -1, D)
             paths = ancestors(self.parents[b])
             for i, path in enumerate(paths):
@@ -133,8 +134,11 @@ class Setup:
                     row = self.cu[b] + i
                     out[row, hq], lse[row, hq], mass[row, hq] = p @ vv, total, p @ vv.abs()
                     # D binary32 additions, each off by at most 2^-23 (the adder may truncate) of the sum of magnitudes
-                    ds[row, hq] = D * 2.0 ** -23 * scale * (kk.abs() @ qq.abs()).max()
-        return out, lse, mass, ds
+                    # + what is left of q: 2^-18 of its largest element
+                    ds[row, hq] = scale * (D * 2.0 ** -23 * (kk.abs() @ qq.abs()).max() + 2.0 ** -18 * qq.abs().max() * kk.abs().sum(1).max())
+                    vmax = self.vs[pages][:, hq // rep].double().max()
+                    floor[row, hq] = 2.0 ** -19 * p.max() * vmax * code[hq // rep][keys].abs().sum(0)
+        return out, lse, mass, ds, floor
 
     def append(self, rope=True):
         """Expected (q, k values, v values, k_scale, v_scale, bytes that change): k / v values are code-space reals before

@@ -4,8 +4,12 @@ Tolerances.  A result rounded to a type is off by at most half a step of it (2^-
 normal e4m3 code, half of 2^-9 below its normal range); what stands in front of that rounding is binary32:
   norm    a sum of H squares in a tree of fewer than 64 sequential steps, a root, two products: 2^-17 of the value
   linear  exact products, K + 8 additions: (K + 8) 2^-23 sum |x w| (2^-23: the tensor core's adder may truncate)
-  attend  probabilities rounded to f16 (2^-11) and off by the scores' error (exponent: twice ds), binary32 sums over the
-          keys and chunks: (2^-11 + 2^-14 + 4 ds) sum p |v|;  lse: 2 ds + 2^-19 (1 + |lse|)
+  attend  a probability is kept as two e4m3 terms, the second one of 16 times what the first leaves: half a step of half
+          a step, 2^-4 2^-4 = 2^-8 of it, after a rounding to f16 (2^-11); below the first term's normal range the second's
+          smallest half step counts, 2^-10 / 16, in units in which the row's largest p is 2^5 or more and the chunk's largest
+          V scale is 1: 2^-19 pmax vmax |code| per key (`floor`).  The scores' error (ds, an exponent) counts twice, on p and
+          on the sum; binary32 sums over keys and chunks 2^-14: (2^-8 + 2^-11 + 2^-14 + 4 ds) sum p |v| + floor.
+          q in three e4m3 terms is off by 2^-18 of its row's largest element or less: part of ds.  lse: 2 ds + 2^-19 (1 + |lse|)
   append  rotation in binary32: 2^-22 of the two products' magnitudes
 """
 import pytest
@@ -159,6 +163,10 @@ def device_cache(s):
     return c, d
 
 
+def p_tol(mass, ds, floor):
+    return (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -14 + 4 * ds)[..., None] * mass + floor
+
+
 def attend_case(s, window=0, sinks=None, scale=None):
     c, d = device_cache(s)
     out = torch.full((s.T, s.heads * s.rep, s.D), 7.0, dtype=BF16, device="cuda")
@@ -166,9 +174,9 @@ def attend_case(s, window=0, sinks=None, scale=None):
     moev.cache_attend(c, d, s.q.cuda(), out, lse=lse, scale=scale, window=window, sinks=None if sinks is None else sinks.cuda())
     torch.cuda.synchronize()
     assert int(d.status) == 0
-    ref, lref, mass, ds = s.attend(window, sinks, scale)
+    ref, lref, mass, ds, floor = s.attend(window, sinks, scale)
     live = s.cu[-1]
-    close(out[:live], ref[:live], R.HALF[BF16] * (1 + 2.0 ** -7) * ref[:live].abs() + ((2.0 ** -11 + 2.0 ** -14 + 4 * ds)[..., None] * mass)[:live] + 1e-30, "out")
+    close(out[:live], ref[:live], R.HALF[BF16] * (1 + 2.0 ** -7) * ref[:live].abs() + p_tol(mass, ds, floor)[:live] + 1e-30, "out")
     close(lse[:live], lref[:live], (2 * ds + 2.0 ** -19 * (1 + lref.abs()))[:live], "lse")
     assert (out[live:] == 7).all() and (lse[live:] == 7).all()
 
@@ -315,9 +323,9 @@ def test_append_then_attend_is_attention_over_the_appended_tokens():
         q = moev.cache_append(c, d, s.nk.cuda(), s.nv.cuda(), rope=s.rope.cuda(), q=s.q.cuda())
         out = moev.cache_attend(c, d, q)
         s.k, s.v, s.ks, s.vs, s.q = c.k.cpu(), c.v.cpu(), c.k_scale.cpu(), c.v_scale.cpu(), q.cpu()
-        ref, _, mass, ds = s.attend()
+        ref, _, mass, ds, floor = s.attend()
         live = s.cu[-1]
-        close(out[:live], ref[:live], R.HALF[BF16] * (1 + 2.0 ** -7) * ref[:live].abs() + ((2.0 ** -11 + 2.0 ** -14 + 4 * ds)[..., None] * mass)[:live], "out")
+        close(out[:live], ref[:live], R.HALF[BF16] * (1 + 2.0 ** -7) * ref[:live].abs() + p_tol(mass, ds, floor)[:live], "out")
         s.ctx = [a + b for a, b in zip(s.ctx, (2, 0, 5))]
 
 
