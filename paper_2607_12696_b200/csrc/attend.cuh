@@ -8,25 +8,24 @@
 // products have the cache as the A operand of tcgen05.mma (128 wide whatever the rows) and the rows as the narrow
 // one, N = R = 16, 32, 64 or 128:
 //   S^T [128 keys, R]  = K tile [128 keys, D] . Q^T          O^T [D, R] += V^T tile [D, 128 keys] . P^T
-// so the e4m3 codes go from the cache by TMA to shared memory and from there to the multiplier as they are; a page
-// is stored in the order in which the instruction reads it (K by token, V by dimension), a tile is 128 / page pages
-// side by side, each in the swizzle of its row length.  kind::f8f6f4 wants 8-bit operands on both sides:
-//   q (bf16): three e4m3 terms of q * 2^e, largest element in [128, 256): each term takes the rest of the one before;
-//     what is left is 2^-18 of the row's largest element or 2^-12 of the element, whichever is more.  They add in one accumulator.
-//   p: two terms, hi = e4m3(p), lo = e4m3(16 (p - hi)), in accumulators of their own, O = O_hi + O_lo / 16: off by 2^-8
-//     of p at most (half a step of half a step; 7e-4 in the mean square, under bf16's own 1.7e-3 of the output) down to
-//     2^-12 of the row's maximum, and by 2^-20 of the maximum below that.
+// K codes go from the cache by TMA to shared memory and from there to the multiplier as they are (a tile is 128 / page
+// pages side by side); kind::f8f6f4 wants 8-bit operands on both sides, so q (bf16) is three e4m3 terms of q * 2^e, its
+// largest element in [128, 256): each term takes the rest of the one before, what is left is 2^-18 of the row's largest
+// element or 2^-12 of the element, whichever is more.  They add in one accumulator.
+// The second product runs in kind::f16: V codes, exact in f16, are widened on the way (16 KB of codes per tile, whatever
+// R), and p is rounded once to f16 (2^-11).  In 8 bits p would need two terms and leave the reference below 3 bits of room.
 // The scale of a page's K multiplies its scores, that of its V the probabilities relative to the largest V scale of late.
 //
 // In S^T a thread is a key (one page, one scale) and its registers are rows, so a maximum over keys would go across
-// lanes.  It is not taken: the reference m_r only has to be near it.  p = 2^(s - m_r) may reach 2^3 (times 2^5 it still
-// fits e4m3); only when some score exceeds that (always in the first tile, then rarely) the CTA takes the
-// maxima, moves m_r and rescales O and the denominators.  Those are per thread, summed across lanes once at the end.
+// lanes.  It is not taken: the reference m_r only has to be near it.  p = 2^(s - m_r) may reach 2^14 in f16; only
+// when some score exceeds that (in the first tile, then hardly ever) the CTA takes the maxima, moves m_r and rescales
+// O and the denominators.  Those are per thread, summed across lanes once at the end.
 //
-// Roles: one warp loads (TMA), one thread issues the MMAs, eight warps do the softmax, four for each half of the
-// rows (tensor memory gives a warp a quarter of the lanes).  S and P are double-buffered: S of tile i + 1 is
-// computed while the softmax works on tile i.  Work split: grid = (chunks of the key range, kv head x row tiles,
-// sequence); chunks meet in a second kernel (attend_combine), in order.  Every wait is bounded.
+// Roles: one warp loads (TMA), one thread issues the MMAs, eight warps do the softmax and widen V, four for each half of
+// the rows (tensor memory gives a warp a quarter of the lanes).  S is double-buffered: S of tile i + 1 is computed
+// while the softmax works on tile i, the second product of tile i while it works on tile i + 1.  Work split: grid =
+// (chunks of the key range, kv head x row tiles, sequence); chunks meet in a second kernel (attend_combine), in order.
+// Every wait is bounded.
 #pragma once
 #include <cuda.h>
 
@@ -42,8 +41,7 @@ using kv::Seq;
 
 constexpr int kKeys = 128;                 // keys of a tile
 constexpr int kThreads = 320;              // 8 softmax warps, loader, MMA issuer
-constexpr float kLimit = 3.f;              // scores may exceed the reference by this many powers of two ...
-constexpr float kUp = 32.f, kDown = 1.f / 32.f;  // ... and p is kept times 2^5: 2^8 < 448
+constexpr float kLimit = 14.f;             // scores may exceed the reference by this many powers of two
 constexpr float kUnseen = -3.0e38f;        // reference of a row that has not seen a key yet
 constexpr unsigned long long kBudgetNs = 2000000000ull;
 
@@ -96,16 +94,11 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                "r"(bytes), "r"(ptx::smem_u32(bar))
                : "memory");
 }
-// two f16 -> two e4m3 codes (saturating) and back
-__device__ __forceinline__ uint32_t f16_to_codes(uint32_t h) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
-  return r;
-}
-__device__ __forceinline__ uint32_t codes_to_f16(uint32_t c) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)c));
-  return r;
+// four e4m3 codes -> two f16 pairs
+__device__ __forceinline__ void codes_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(w));
 }
 
 // First key of the range that a sequence's drafts can see (a multiple of 128).
@@ -138,32 +131,33 @@ template <int D, int R>
 struct Cfg {
   static constexpr int kCtas = R <= 32 ? 2 : 1;  // per SM
   static constexpr int kTile = kKeys * D;        // bytes of a K or V tile
-  static constexpr int kStages = D == 128 ? (R <= 32 ? 2 : R == 64 ? 4 : 3) : (R <= 32 ? 4 : 6);
-  static constexpr int kP = R * kKeys;           // bytes of one term of P
+  static constexpr int kKStages = D == 128 && R <= 32 ? 2 : 3;
+  static constexpr int kVStages = D == 128 && R <= 32 ? 1 : 2;
+  static constexpr int kP = R * kKeys * 2;       // bytes of P and of the widened V tile, two blocks of 64 keys each
+  static constexpr int kV16 = D * kKeys * 2;
   static constexpr int kQ = R * D;
-  static constexpr int kTmem = 4 * R;            // S x 2, O_hi, O_lo
-  // byte offsets
-  static constexpr int oK = 0, oV = kStages * kTile, oP = 2 * kStages * kTile, oQ = oP + 4 * kP, oCtl = oQ + 3 * kQ;
+  static constexpr int kTmem = R == 128 ? 512 : 4 * R;  // S x 2, O
+  // byte offsets (O has 128 lanes: with D = 64 the upper ones come from what lies behind the V tile, and are not used)
+  static constexpr int oK = 0, oV = kKStages * kTile, oV16 = oV + kVStages * kTile, oP = oV16 + kV16, oQ = oP + kP, oCtl = oQ + 3 * kQ;
+  static_assert(D == 128 || kP + 3 * kQ + 2048 >= kV16 / 2, "reads behind the V tile stay in the buffer");
 };
 
 template <int R>
 struct Ctl {
-  static constexpr int kMaxStages = 6;
-  uint64_t k_full[kMaxStages], k_empty[kMaxStages], v_full[kMaxStages], v_empty[kMaxStages];
-  uint64_t s_full[2], s_empty[2], p_full[2], p_empty[2], drain;
+  uint64_t k_full[3], k_empty[3], v_full[2], v_empty[2];
+  uint64_t s_full[2], s_empty[2], p_full, o_full, q_full, drain;
   alignas(16) float2 rcm[R];    // row's factor from raw scores to powers of two | its reference m
   float fac_l[R], fac_o[R];
   float wmax[4][R], lsum[4][R];
-  float ks[kMaxStages][8], vs[kMaxStages][8];  // scales of a tile's 16-key pieces
-  int pid[kMaxStages][8];
-  uint32_t vis[R][4];           // draft of the tile sees key (bits)
-  uint32_t nan_key[kKeys][4], nan_row[R][4];
+  float ks[2][8], vs[2][8];     // by V stage: scales of a tile's 16-key pieces
+  int pid[2][8];                // and their pages
+  uint32_t vis[2][R][4];        // by tile parity: draft of the tile sees key (bits)
+  uint32_t nan_row[R][4];       // row's output is NaN in these dimensions
   int low[R], top[R];           // by draft of the tile: context keys > low are seen; a chain sees keys <= top
   int2 row[R];                  // token row, query head; -1: no row
   uint32_t tmem;
   volatile int abort;
   volatile uint32_t k_it, v_it;  // tiles the loader armed (read on the abort path)
-  int nan_any;
 };
 template <int D, int R>
 size_t smem_bytes(int words, bool tree) {  // + ancestor words of the tile's drafts, parents of the sequence
@@ -190,29 +184,31 @@ template <int D, int R>
 __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(const Args a, const __grid_constant__ CUtensorMap tm_k,
                                                                             const __grid_constant__ CUtensorMap tm_v) {
   using C = Cfg<D, R>;
-  constexpr int ST = C::kStages, RH = R / 2;
+  constexpr int KS = C::kKStages, VS = C::kVStages, RH = R / 2;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   Ctl<R>& S = *reinterpret_cast<Ctl<R>*>(smem + C::oCtl);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int i = 0; i < ST; ++i) {
+    for (int i = 0; i < KS; ++i) {
       ptx::mbar_init(&S.k_full[i], 1);
       ptx::mbar_init(&S.k_empty[i], 1);
+    }
+    for (int i = 0; i < VS; ++i) {
       ptx::mbar_init(&S.v_full[i], 1);
-      ptx::mbar_init(&S.v_empty[i], 1);
+      ptx::mbar_init(&S.v_empty[i], 8);
     }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&S.s_full[i], 1);
       ptx::mbar_init(&S.s_empty[i], 8);
-      ptx::mbar_init(&S.p_full[i], 8);
-      ptx::mbar_init(&S.p_empty[i], 1);
     }
+    ptx::mbar_init(&S.p_full, 8);
+    ptx::mbar_init(&S.o_full, 1);
+    ptx::mbar_init(&S.q_full, 1);
     ptx::mbar_init(&S.drain, 1);
     ptx::fence_mbar_init();
     S.abort = 0;
     S.k_it = S.v_it = 0;
-    S.nan_any = 0;
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   // Tensor memory is taken behind the wait and dependents are released behind that: no kernel holds tensor memory while
@@ -258,53 +254,50 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
       };
       int pid = page_at(0);
       for (int it = 0; it < n_tiles; ++it) {
-        const int st = it % ST;
-        const uint32_t parity = ((it / ST) & 1) ^ 1;
+        const int sk = it % KS, sv = it % VS;
         const int next = page_at(it + 1);
         const int mine = __shfl_sync(0xffffffffu, pid, ((lane & 7) << page_log2) >> 4 & 7);  // page `lane` of the tile
         const bool on = lane < pages && mine >= 0;
         const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, on)) * page * D;
-        if (it >= ST && __any_sync(0xffffffffu, !wait(&S.k_empty[st], parity, &S.abort, a.d.status))) break;
-        uint8_t* dst = smem + C::oK + st * C::kTile + (lane & 7) * page * D;
+        if (it >= KS && __any_sync(0xffffffffu, !wait(&S.k_empty[sk], ((it / KS) & 1) ^ 1, &S.abort, a.d.status))) break;
+        uint8_t* dst = smem + C::oK + sk * C::kTile + (lane & 7) * page * D;
         if (lane == 0) {
-          ptx::mbar_arrive_expect_tx(&S.k_full[st], bytes);
+          ptx::mbar_arrive_expect_tx(&S.k_full[sk], bytes);
           S.k_it = it + 1;
         }
         __syncwarp();
-        if (on) ptx::tma_load_2d(dst, &tm_k, &S.k_full[st], 0, (mine * a.c.heads + head) << page_log2, ptx::kPolicyEvictNormal);
-        if (it >= ST && __any_sync(0xffffffffu, !wait(&S.v_empty[st], parity, &S.abort, a.d.status))) break;
+        if (on) ptx::tma_load_2d(dst, &tm_k, &S.k_full[sk], 0, (mine * a.c.heads + head) << page_log2, ptx::kPolicyEvictNormal);
+        if (it >= VS && __any_sync(0xffffffffu, !wait(&S.v_empty[sv], ((it / VS) & 1) ^ 1, &S.abort, a.d.status))) break;
         if (lane < 8) {
           const long long slot = (long long)max(pid, 0) * a.c.heads + head;
-          S.ks[st][lane] = pid >= 0 ? a.c.ks[slot] : 0.f;
-          S.vs[st][lane] = pid >= 0 ? a.c.vs[slot] : 0.f;
-          S.pid[st][lane] = pid;
+          S.ks[sv][lane] = pid >= 0 ? a.c.ks[slot] : 0.f;
+          S.vs[sv][lane] = pid >= 0 ? a.c.vs[slot] : 0.f;
+          S.pid[sv][lane] = pid;
         }
         __syncwarp();
         if (lane == 0) {
-          ptx::mbar_arrive_expect_tx(&S.v_full[st], bytes);
+          ptx::mbar_arrive_expect_tx(&S.v_full[sv], bytes);
           S.v_it = it + 1;
         }
         __syncwarp();
-        dst += C::oV - C::oK;
+        dst = smem + C::oV + sv * C::kTile + (lane & 7) * page * D;
         if (on) {
-          if (page_log2 == 4) bulk_load(dst, a.c.v + ((long long)mine * a.c.heads + head) * (D * 16), D * 16, &S.v_full[st]);
-          else ptx::tma_load_2d(dst, &tm_v, &S.v_full[st], 0, (mine * a.c.heads + head) * D, ptx::kPolicyEvictNormal);
+          if (page_log2 == 4) bulk_load(dst, a.c.v + ((long long)mine * a.c.heads + head) * (D * 16), D * 16, &S.v_full[sv]);
+          else ptx::tma_load_2d(dst, &tm_v, &S.v_full[sv], 0, (mine * a.c.heads + head) * D, ptx::kPolicyEvictNormal);
         }
         pid = next;
       }
     } else if (warp == 9) {
       // ------------------------------------------------------------ MMA issuer
       if (lane == 0) {
-        const uint32_t idesc = ptx::instr_desc(0, 0, R);
-        const uint32_t kb = ptx::smem_u32(smem + C::oK), vb = ptx::smem_u32(smem + C::oV), pb = ptx::smem_u32(smem + C::oP),
+        const uint32_t idesc = ptx::instr_desc(0, 0, R);  // e4m3 x e4m3 in kind::f8f6f4, f16 x f16 in kind::f16
+        const uint32_t kb = ptx::smem_u32(smem + C::oK), vb = ptx::smem_u32(smem + C::oV16), pb = ptx::smem_u32(smem + C::oP),
                        qb = ptx::smem_u32(smem + C::oQ);
         constexpr uint32_t kLay = D == 128 ? kSw128 : kSw64;
-        const uint32_t v_lay = page_log2 == 7 ? kSw128 : page_log2 == 6 ? kSw64 : page_log2 == 5 ? kSw32 : kSwNone;
-        const uint32_t v_str = page_log2 == 4 ? 128u : 8u << page_log2, v_lead = page_log2 == 4 ? D * 16 : 16;
         bool ok = true;
         auto scores = [&](int it) {
-          const int st = it % ST, u = it & 1;
-          ok = ok && wait(&S.k_full[st], (it / ST) & 1, &S.abort, a.d.status);
+          const int st = it % KS, u = it & 1;
+          ok = ok && wait(&S.k_full[st], (it / KS) & 1, &S.abort, a.d.status);
           if (it >= 2) ok = ok && wait(&S.s_empty[u], ((it >> 1) & 1) ^ 1, &S.abort, a.d.status);
           if (!ok) return;
           ptx::tc_fence_after();
@@ -318,30 +311,22 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
           ptx::mma_commit(&S.s_full[u]);
         };
         if (n_tiles > 0) {
-          ok = wait(&S.drain, 0, &S.abort, a.d.status);  // Q is there
+          ok = wait(&S.q_full, 0, &S.abort, a.d.status);
           scores(0);
         }
         for (int it = 0; it < n_tiles && ok; ++it) {
           if (it + 1 < n_tiles) scores(it + 1);
-          const int st = it % ST, u = it & 1;
-          ok = ok && wait(&S.v_full[st], (it / ST) & 1, &S.abort, a.d.status);
-          ok = ok && wait(&S.p_full[u], (it >> 1) & 1, &S.abort, a.d.status);
+          ok = ok && wait(&S.p_full, it & 1, &S.abort, a.d.status);
           if (!ok) break;
           ptx::tc_fence_after();
 #pragma unroll
-          for (int term = 0; term < 2; ++term)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t step = page_log2 == 7 ? k * 32 : page_log2 == 6 ? (k >> 1) * (D * 64) + (k & 1) * 32 : k * (D * 32);
-              ptx::mma_f8f6f4(tmem + (2 + term) * R, desc_of(vb + st * C::kTile + step, v_lead, v_str, v_lay),
-                              desc_of(pb + (2 * u + term) * C::kP + k * 32, 16, 1024, kSw128), idesc, it + k > 0);
-            }
-          ptx::mma_commit(&S.v_empty[st]);
-          ptx::mma_commit(&S.p_empty[u]);
+          for (int k = 0; k < kKeys / 16; ++k)
+            ptx::mma_f16(tmem + 2 * R, desc_of(vb + (k >> 2) * (C::kV16 / 2) + (k & 3) * 32, 16, 1024, kSw128),
+                         desc_of(pb + (k >> 2) * (C::kP / 2) + (k & 3) * 32, 16, 1024, kSw128), idesc, it + k > 0);
+          ptx::mma_commit(&S.o_full);
         }
         if (!ok) {  // abort: what was issued must have ended before tensor memory and shared memory are given back
-          ptx::mma_commit(&S.drain);
-          ptx::drain_wait(&S.drain, 1, kBudgetNs);
+          ptx::drain_issuer(&S.drain, kBudgetNs);
         }
       }
     } else {
@@ -411,29 +396,21 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
       }
       ptx::fence_proxy_async_smem();
       ptx::named_barrier(2, 256);
-      if (tid == 0) ptx::mbar_arrive(&S.drain);
+      if (tid == 0) ptx::mbar_arrive(&S.q_full);
 
       float l[RH];
 #pragma unroll
       for (int r = 0; r < RH; ++r) l[r] = 0.f;
       float u = 0.f;  // V scale that the accumulators are in units of
       const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-      uint32_t xo[8];  // this key's byte in row r of P: (r & 7) selects
+      uint32_t xo[8];  // this key's place in row r of P: (r & 7) selects
 #pragma unroll
-      for (int k = 0; k < 8; ++k) xo[k] = (((key >> 4) ^ k) << 4) + (key & 15);
+      for (int k = 0; k < 8; ++k) xo[k] = (key >> 6) * (C::kP / 2) + ((((key & 63) >> 3) ^ k) << 4) + (key & 7) * 2 + r0 * 128;
       bool ok = true;
       for (int it = 0; it < n_tiles; ++it) {
-        const int st = it % ST, bu = it & 1;
+        const int sv = it % VS, bu = it & 1;
         const int k0 = k_begin + it * kKeys;
-        ok = wait(&S.v_full[st], (it / ST) & 1, &S.abort, a.d.status) && ok;
-        // a thread that gave up stays with the others' barriers until here, where all of them leave
-        if (any_of_256(!ok)) {
-          ok = false;
-          break;
-        }
-        bool masked = k0 + kKeys > s.ctx || k0 <= low_max;  // somebody may not see a key of the tile
-#pragma unroll
-        for (int e = 0; e < 8; ++e) masked = masked || S.pid[st][e] < 0;
+        const bool masked = k0 + kKeys > s.ctx || k0 <= low_max;  // somebody may not see a key of the tile
         if (masked) {
           // what each draft of the tile sees of its keys
           for (int z = tid; z < (i_last - i_first + 1) * 4; z += 256) {
@@ -446,90 +423,70 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
               if (off < 0) bits |= an[0] << -off;
               else bits |= __funnelshift_r(an[off >> 5], (off >> 5) + 1 < words ? an[(off >> 5) + 1] : 0u, off & 31);
             }
-            // pages that are not there
-            if (S.pid[st][2 * (z & 3)] < 0) bits &= 0xffff0000u;
-            if (S.pid[st][2 * (z & 3) + 1] < 0) bits &= 0x0000ffffu;
-            S.vis[dr][z & 3] = bits;
-          }
-          for (int z = tid; z < kKeys * 4; z += 256) (&S.nan_key[0][0])[z] = 0;
-          if (tid == 0) S.nan_any = 0;
-          ptx::named_barrier(2, 256);
-          // V of keys behind the end or without a page becomes zero, so that 0 * V is 0; a NaN of a written key is taken out
-          // too and kept as bits, for the rows that do see the key
-          uint8_t* vt = smem + C::oV + st * C::kTile;
-          for (int z = tid; z < D * 8; z += 256) {
-            const int d = z >> 3, seg = z & 7;
-            const int have = S.pid[st][seg] < 0 ? 0 : min(16, max(0, k_all - (k0 + 16 * seg)));
-            uint4* at = reinterpret_cast<uint4*>(vt + v_piece<D>(d, seg, page_log2));
-            uint4 w = have > 0 ? *at : make_uint4(0, 0, 0, 0);
-            uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-            bool changed = have < 16;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int keep = min(4, max(0, have - 4 * e));
-              if (keep < 4) ww[e] &= keep == 0 ? 0u : 0xffffffffu >> (32 - 8 * keep);
-              uint32_t bad = __vcmpeq4(ww[e] & 0x7f7f7f7fu, 0x7f7f7f7fu);
-              if (bad) {
-                ww[e] &= ~bad;
-                changed = true;
-                S.nan_any = 1;
-                for (int y = 0; y < 4; ++y)
-                  if ((bad >> (8 * y)) & 1u) atomicOr(&S.nan_key[seg * 16 + 4 * e + y][d >> 5], 1u << (d & 31));
-              }
-            }
-            if (changed) *at = make_uint4(ww[0], ww[1], ww[2], ww[3]);
+            S.vis[bu][dr][z & 3] = bits;
           }
           ptx::named_barrier(2, 256);
-          if (S.nan_any) {
-            uint32_t nk[4];
-#pragma unroll
-            for (int y = 0; y < 4; ++y) nk[y] = S.nan_key[key][y];
-            if (nk[0] | nk[1] | nk[2] | nk[3])
-              for (int r = r0; r < r0 + RH; ++r)
-                if (row0 + r < n_rows && (S.vis[(row0 + r) / a.rep - i_first][key >> 5] >> (key & 31)) & 1u)
-                  for (int y = 0; y < 4; ++y)
-                    if (nk[y]) atomicOr(&S.nan_row[r][y], nk[y]);
-          }
         }
+        ok = wait(&S.v_full[sv], (it / VS) & 1, &S.abort, a.d.status) && ok;
         ok = wait(&S.s_full[bu], (it >> 1) & 1, &S.abort, a.d.status) && ok;
         ptx::tc_fence_after();
-        float v[RH];
-#pragma unroll
-        for (int c = 0; c < RH / 8; ++c) tmem_ld8(tmem + lane_base + bu * R + r0 + 8 * c, *reinterpret_cast<uint32_t(*)[8]>(&v[8 * c]));
-        ptx::tmem_ld_wait();
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&S.s_empty[bu]);
-
-        const float k_scale = S.ks[st][key >> 4], v_scale = S.vs[st][key >> 4];
+        const float k_scale = S.ks[sv][key >> 4], v_scale = S.vs[sv][key >> 4];
+        const bool there = S.pid[sv][key >> 4] >= 0;
         float vm = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vm = fmaxf(vm, S.vs[st][e]);
-        const bool unit = vm > u || vm < u * (1.f / 64.f);  // the same in every thread
+        for (int e = 0; e < 8; ++e) vm = fmaxf(vm, S.vs[sv][e]);
+        float v[RH];
+        auto load_scores = [&]() {  // times the page's scale; -inf where the row does not see this thread's key
 #pragma unroll
-        for (int r = 0; r < RH; ++r) v[r] *= k_scale;
-        if (masked) {
+          for (int c = 0; c < RH / 8; ++c) tmem_ld8(tmem + lane_base + bu * R + r0 + 8 * c, *reinterpret_cast<uint32_t(*)[8]>(&v[8 * c]));
+          ptx::tmem_ld_wait();
 #pragma unroll
-          for (int r = 0; r < RH; ++r) {
-            const int rr = min(row0 + r0 + r, n_rows - 1);
-            if (!((S.vis[rr / a.rep - i_first][quad] >> lane) & 1u)) v[r] = -INFINITY;
+          for (int r = 0; r < RH; ++r) v[r] *= k_scale;
+          if (masked) {
+            int dr = (row0 + r0) / a.rep, in = row0 + r0 - dr * a.rep;  // row's draft and its head
+            dr -= i_first;
+            uint32_t bits = S.vis[bu][min(dr, i_last - i_first)][quad];
+#pragma unroll
+            for (int r = 0; r < RH; ++r) {
+              if (!((bits >> lane) & 1u)) v[r] = -INFINITY;
+              if (++in == a.rep) {
+                in = 0;
+                ++dr;
+                bits = S.vis[bu][min(dr, i_last - i_first)][quad];
+              }
+            }
           }
-        }
-        float tmax = -INFINITY;
+          if (!there) {
 #pragma unroll
-        for (int r = 0; r < RH; ++r) {
-          const float2 q = S.rcm[r0 + r];
-          tmax = fmaxf(tmax, fmaf(v[r], q.x, -q.y));
+            for (int r = 0; r < RH; ++r) v[r] = -INFINITY;
+          }
+        };
+        load_scores();
+        float tmax = ok ? -INFINITY : INFINITY;
+#pragma unroll
+        for (int r = 0; r < RH; r += 2) {
+          const float4 q = *reinterpret_cast<const float4*>(&S.rcm[r0 + r]);
+          v[r] = fmaf(v[r], q.x, -q.y);
+          v[r + 1] = fmaf(v[r + 1], q.z, -q.w);
+          tmax = fmaxf(tmax, fmaxf(v[r], v[r + 1]));
         }
-        if (any_of_256(tmax > kLimit || (unit && vm > 0.f))) {
-          // move the references to the maxima and the unit to the tile's largest V scale
+        const bool unit = vm > 0.f && (vm > u || vm < u * (1.f / 64.f));  // the same in every thread
+        if (any_of_256(tmax > kLimit || unit)) {
+          if (any_of_256(!ok)) {  // a thread that gave up stays with the others' barriers until here: all of them leave
+            ok = false;
+            break;
+          }
+          // move the references to the maxima and the unit to the tile's largest V scale.  From the scores themselves:
+          // relative to the reference of a row that has seen nothing they have lost their digits
+          load_scores();
 #pragma unroll
           for (int r = 0; r < RH; ++r) {
-            const float m = warp_max(v[r] * S.rcm[r0 + r].x);
+            v[r] *= S.rcm[r0 + r].x;
+            const float m = warp_max(v[r]);
             if (lane == 0) S.wmax[quad][r0 + r] = m;
           }
           ptx::named_barrier(2, 256);
-          const float u_new = unit && vm > 0.f ? vm : u;
+          const float u_new = unit ? vm : u;
           if (tid < R) {
             const float old = S.rcm[tid].y;
             const float m = fmaxf(fmaxf(old, fmaxf(S.wmax[0][tid], S.wmax[1][tid])), fmaxf(S.wmax[2][tid], S.wmax[3][tid]));
@@ -541,51 +498,94 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
           ptx::named_barrier(2, 256);
           u = u_new;
 #pragma unroll
-          for (int r = 0; r < RH; ++r) l[r] *= S.fac_l[r0 + r];
+          for (int r = 0; r < RH; ++r) {
+            l[r] *= S.fac_l[r0 + r];
+            v[r] -= S.rcm[r0 + r].y;
+          }
           if (it > 0) {
-            ok = wait(&S.p_empty[bu ^ 1], ((it - 1) >> 1) & 1, &S.abort, a.d.status) && ok;  // the product of tile it - 1 has ended
+            ok = wait(&S.o_full, (it - 1) & 1, &S.abort, a.d.status) && ok;  // the second product of tile it - 1 has ended
             ptx::tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < RH / 8; ++c)
+            for (int c = 0; c < RH / 8; ++c) {
+              uint32_t o[8];
+              const uint32_t at = tmem + lane_base + 2 * R + r0 + 8 * c;
+              tmem_ld8(at, o);
+              ptx::tmem_ld_wait();
 #pragma unroll
-              for (int term = 0; term < 2; ++term) {
-                uint32_t o[8];
-                const uint32_t at = tmem + lane_base + (2 + term) * R + r0 + 8 * c;
-                tmem_ld8(at, o);
-                ptx::tmem_ld_wait();
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * S.fac_o[r0 + 8 * c + e]);
-                tmem_st8(at, o);
-              }
+              for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * S.fac_o[r0 + 8 * c + e]);
+              tmem_st8(at, o);
+            }
             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
             ptx::tc_fence_before();
           }
         }
-        if (it >= 2) ok = wait(&S.p_empty[bu], ((it >> 1) & 1) ^ 1, &S.abort, a.d.status) && ok;
-        const float f = u > 0.f ? v_scale / u * kUp : 0.f;
-        uint8_t* ph = smem + C::oP + (2 * bu) * C::kP + r0 * 128;
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&S.s_empty[bu]);
+        const __half2 f = __float2half2_rn(u > 0.f ? v_scale / u : 0.f);
+        uint32_t p[RH / 2];
 #pragma unroll
         for (int r = 0; r < RH; r += 2) {
-          const float4 q = *reinterpret_cast<const float4*>(&S.rcm[r0 + r]);
-          const float p0 = exp2_fast(fmaf(v[r], q.x, -q.y)), p1 = exp2_fast(fmaf(v[r + 1], q.z, -q.w));
+          const float p0 = exp2_fast(v[r]), p1 = exp2_fast(v[r + 1]);
           l[r] += p0;
           l[r + 1] += p1;
-          const __half2 h = __floats2half2_rn(p0 * f, p1 * f);
-          const uint32_t hi = f16_to_codes(*reinterpret_cast<const uint32_t*>(&h));
-          const uint32_t bk = codes_to_f16(hi);
-          const __half2 rest = __hmul2(__hsub2(h, *reinterpret_cast<const __half2*>(&bk)), __half2half2(__ushort_as_half(0x4C00)));  // * 16
-          const uint32_t lo = f16_to_codes(*reinterpret_cast<const uint32_t*>(&rest));
-          ph[r * 128 + xo[r & 7]] = (uint8_t)hi;
-          ph[(r + 1) * 128 + xo[(r + 1) & 7]] = (uint8_t)(hi >> 8);
-          ph[C::kP + r * 128 + xo[r & 7]] = (uint8_t)lo;
-          ph[C::kP + (r + 1) * 128 + xo[(r + 1) & 7]] = (uint8_t)(lo >> 8);
+          const __half2 h = __hmul2(__floats2half2_rn(p0, p1), f);
+          p[r / 2] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        // P and the widened V are free once the second product of the tile before has ended
+        if (it > 0) ok = wait(&S.o_full, (it - 1) & 1, &S.abort, a.d.status) && ok;
+        uint8_t* pt = smem + C::oP;
+#pragma unroll
+        for (int r = 0; r < RH; r += 2) {
+          *reinterpret_cast<uint16_t*>(pt + r * 128 + xo[r & 7]) = (uint16_t)p[r / 2];
+          *reinterpret_cast<uint16_t*>(pt + (r + 1) * 128 + xo[(r + 1) & 7]) = (uint16_t)(p[r / 2] >> 16);
+        }
+        const uint8_t* vt = smem + C::oV + sv * C::kTile;
+        uint8_t* wt = smem + C::oV16;
+#pragma unroll
+        for (int z0 = 0; z0 < D * 8; z0 += 256) {
+          const int z = z0 + tid, d = z >> 3, seg = z & 7;
+          const uint4 w = *reinterpret_cast<const uint4*>(vt + v_piece<D>(d, seg, page_log2));
+          uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+          if (masked || S.pid[sv][seg] < 0) {
+            // keys behind the end or without a page count as zero, so that 0 * V is 0; a NaN of a written key goes to the
+            // rows that see the key, and to no others
+            const int have = S.pid[sv][seg] < 0 ? 0 : min(16, max(0, k_all - (k0 + 16 * seg)));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int keep = min(4, max(0, have - 4 * e));
+              if (keep < 4) ww[e] &= keep == 0 ? 0u : 0xffffffffu >> (32 - 8 * keep);
+              const uint32_t bad = __vcmpeq4(ww[e] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+              if (masked && bad) {
+                ww[e] &= ~bad;
+                for (int y = 0; y < 4; ++y)
+                  if ((bad >> (8 * y)) & 1u) {
+                    const int kk = seg * 16 + 4 * e + y;
+                    for (int r = 0; r < R && row0 + r < n_rows; ++r)
+                      if ((S.vis[bu][(row0 + r) / a.rep - i_first][kk >> 5] >> (kk & 31)) & 1u) atomicOr(&S.nan_row[r][d >> 5], 1u << (d & 31));
+                  }
+              }
+            }
+          }
+          uint4 x, y;
+          codes_to_f16(ww[0], x.x, x.y);
+          codes_to_f16(ww[1], x.z, x.w);
+          codes_to_f16(ww[2], y.x, y.y);
+          codes_to_f16(ww[3], y.z, y.w);
+          uint8_t* at = wt + (seg >> 2) * (C::kV16 / 2) + d * 128;
+          const int ch = (seg & 3) * 2;
+          *reinterpret_cast<uint4*>(at + ((ch ^ (d & 7)) << 4)) = x;
+          *reinterpret_cast<uint4*>(at + (((ch + 1) ^ (d & 7)) << 4)) = y;
         }
         ptx::fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&S.p_full[bu]);
+        if (lane == 0) {
+          ptx::mbar_arrive(&S.p_full);
+          ptx::mbar_arrive(&S.v_empty[sv]);
+        }
       }
       // ---- results
-      if (ok && n_tiles > 0) ok = wait(&S.p_empty[(n_tiles - 1) & 1], ((n_tiles - 1) >> 1) & 1, &S.abort, a.d.status);
+      if (ok && n_tiles > 0) ok = wait(&S.o_full, (n_tiles - 1) & 1, &S.abort, a.d.status);
       ptx::tc_fence_after();
 #pragma unroll
       for (int r = 0; r < RH; ++r) {
@@ -595,20 +595,18 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
         if (lane == 0) S.lsum[quad][r0 + r] = x;
       }
       if (!any_of_256(!ok)) {
-        const float back = u * kDown;
         const int d = quad * 32 + lane;
         const bool split = a.chunks > 1;
 #pragma unroll 1
         for (int c = 0; c < RH / 8; ++c) {
-          uint32_t oh[8], ol[8];
+          uint32_t oh[8];
           const uint32_t at = tmem + lane_base + 2 * R + r0 + 8 * c;
           if (n_tiles > 0) {
             tmem_ld8(at, oh);
-            tmem_ld8(at + R, ol);
             ptx::tmem_ld_wait();
           } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) oh[e] = ol[e] = 0u;
+            for (int e = 0; e < 8; ++e) oh[e] = 0u;
           }
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
@@ -617,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
             if (ro.x < 0 || d >= D) continue;
             float den = (S.lsum[0][r] + S.lsum[1][r]) + (S.lsum[2][r] + S.lsum[3][r]);
             float m = den == 0.f ? -INFINITY : S.rcm[r].y;
-            float o = (__uint_as_float(oh[e]) + 0.0625f * __uint_as_float(ol[e])) * back;
+            float o = __uint_as_float(oh[e]) * u;
             if ((S.nan_row[r][d >> 5] >> (d & 31)) & 1u) o = __int_as_float(0x7fffffff);
             if (split) {
               const long long w = ((long long)blockIdx.x * a.d.n_tokens + ro.x) * a.n_heads + ro.y;
@@ -639,8 +637,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
       }
     }
     if (S.abort && warp == 8 && lane == 0) {  // copies in flight land before the shared memory is given back
-      ptx::drain_ring(S.k_full, ST, S.k_it, kBudgetNs);
-      ptx::drain_ring(S.v_full, ST, S.v_it, kBudgetNs);
+      ptx::drain_ring(S.k_full, KS, S.k_it, kBudgetNs);
+      ptx::drain_ring(S.v_full, VS, S.v_it, kBudgetNs);
     }
   }
   ptx::tc_fence_before();

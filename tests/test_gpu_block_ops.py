@@ -4,12 +4,12 @@ Tolerances.  A result rounded to a type is off by at most half a step of it (2^-
 normal e4m3 code, half of 2^-9 below its normal range); what stands in front of that rounding is binary32:
   norm    a sum of H squares in a tree of fewer than 64 sequential steps, a root, two products: 2^-17 of the value
   linear  exact products, K + 8 additions: (K + 8) 2^-23 sum |x w| (2^-23: the tensor core's adder may truncate)
-  attend  a probability is kept as two e4m3 terms, the second one of 16 times what the first leaves: half a step of half
-          a step, 2^-4 2^-4 = 2^-8 of it, after a rounding to f16 (2^-11); below the first term's normal range the second's
-          smallest half step counts, 2^-10 / 16, in units in which the row's largest p is 2^5 or more and the chunk's largest
-          V scale is 1: 2^-19 pmax vmax |code| per key (`floor`).  The scores' error (ds, an exponent) counts twice, on p and
-          on the sum; binary32 sums over keys and chunks 2^-14: (2^-8 + 2^-11 + 2^-14 + 4 ds) sum p |v| + floor.
-          q in three e4m3 terms is off by 2^-18 of its row's largest element or less: part of ds.  lse: 2 ds + 2^-19 (1 + |lse|)
+  attend  a probability, its page's V scale relative to a recent largest one and their product are rounded to f16: 3 2^-11;
+          below f16's normal range the smallest half step counts, 2^-25, in units in which the row's largest p is 1 or more
+          and the tile's largest V scale is 2^-6 or more: 2^-19 pmax vmax |code| per key (`floor`).  The scores' error (ds, an
+          exponent) counts twice, on p and on the sum; binary32 sums over keys and chunks 2^-14:
+          (3 2^-11 + 2^-14 + 4 ds) sum p |v| + floor.  q in three e4m3 terms is off by 2^-18 of its row's largest
+          element or less: part of ds.  lse: 2 ds + 2^-19 (1 + |lse|)
   append  rotation in binary32: 2^-22 of the two products' magnitudes
 """
 import pytest
@@ -164,7 +164,7 @@ def device_cache(s):
 
 
 def p_tol(mass, ds, floor):
-    return (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -14 + 4 * ds)[..., None] * mass + floor
+    return (3 * 2.0 ** -11 + 2.0 ** -14 + 4 * ds)[..., None] * mass + floor
 
 
 def attend_case(s, window=0, sinks=None, scale=None):
