@@ -12,17 +12,18 @@
 // pages side by side); kind::f8f6f4 wants 8-bit operands on both sides, so q (bf16) is three e4m3 terms of q * 2^e, its
 // largest element in [128, 256): each term takes the rest of the one before, what is left is 2^-18 of the row's largest
 // element or 2^-12 of the element, whichever is more.  They add in one accumulator.
-// The second product runs in kind::f16: V codes, exact in f16, are widened on the way (16 KB of codes per tile, whatever
-// R), and p is rounded once to f16 (2^-11).  In 8 bits p would need two terms and leave the reference below 3 bits of room.
+// The second product runs in kind::f16: V codes, exact in f16, are widened on their way into tensor memory, which
+// holds the A operand (16 KB of codes per tile, whatever R), and p is rounded once to f16 (2^-11).  In 8 bits p would need
+// two terms and leave the reference below 3 bits of room.
 // The scale of a page's K multiplies its scores, that of its V the probabilities relative to the largest V scale of late.
 //
 // In S^T a thread is a key (one page, one scale) and its registers are rows, so a maximum over keys would go across
-// lanes.  It is not taken: the reference m_r only has to be near it.  p = 2^(s - m_r) may reach 2^14 in f16; only
-// when some score exceeds that (in the first tile, then hardly ever) the CTA takes the maxima, moves m_r and rescales
-// O and the denominators.  Those are per thread, summed across lanes once at the end.
+// lanes.  It is not taken: the reference m_r only has to be near it.  p = 2^(s - m_r) may reach 2^12 in f16; only
+// when some score exceeds that (in the first tile, then hardly ever) the rows' four warps take the maxima, move m_r and
+// rescale O and the denominators.  Those are per thread, summed across lanes once at the end.
 //
-// Roles: one warp loads (TMA), one thread issues the MMAs, eight warps do the softmax and widen V, four for each half of
-// the rows (tensor memory gives a warp a quarter of the lanes).  S is double-buffered: S of tile i + 1 is computed
+// Roles: one warp loads (TMA), one thread issues the MMAs, groups of four warps do the softmax of a share of the rows each
+// (tensor memory gives a warp a quarter of the lanes) and widen V.  S is double-buffered: S of tile i + 1 is computed
 // while the softmax works on tile i, the second product of tile i while it works on tile i + 1.  Work split: grid =
 // (chunks of the key range, kv head x row tiles, sequence); chunks meet in a second kernel (attend_combine), in order.
 // Every wait is bounded.
@@ -40,8 +41,8 @@ using kv::Drafts;
 using kv::Seq;
 
 constexpr int kKeys = 128;                 // keys of a tile
-constexpr int kThreads = 320;              // 8 softmax warps, loader, MMA issuer
-constexpr float kLimit = 14.f;             // scores may exceed the reference by this many powers of two
+// p = 2^(s - m_r) may reach 2^12 and a V scale 8 times the accumulators' unit: 2^15 in f16
+constexpr float kLimit = 12.f, kUnitUp = 8.f, kUnitDown = 1.f / 64.f;
 constexpr float kUnseen = -3.0e38f;        // reference of a row that has not seen a key yet
 constexpr unsigned long long kBudgetNs = 2000000000ull;
 
@@ -64,19 +65,59 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ float warp_max(float v) {
-  float r;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+// Reduces N values (a power of two up to 32) over the warp's lanes: every exchange halves the values a lane holds, N - 1
+// shuffles and a few instead of 5 N.  The lane ends up with value `reduced_index`.
+template <int N, bool MAX>
+__device__ __forceinline__ float warp_reduce(float (&v)[N], int lane) {
+  int o = 16;
+#pragma unroll
+  for (int h = N / 2; h >= 1; h /= 2, o /= 2) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int i = 0; i < h; ++i) {
+      const float keep = up ? v[i + h] : v[i], give = up ? v[i] : v[i + h];
+      const float got = __shfl_xor_sync(0xffffffffu, give, o);
+      v[i] = MAX ? fmaxf(keep, got) : keep + got;
+    }
+  }
+  for (; o >= 1; o /= 2) {
+    const float got = __shfl_xor_sync(0xffffffffu, v[0], o);
+    v[0] = MAX ? fmaxf(v[0], got) : v[0] + got;
+  }
+  return v[0];
+}
+template <int N>
+__device__ __forceinline__ int reduced_index(int lane) {
+  int r = 0, o = 16;
+#pragma unroll
+  for (int h = N / 2; h >= 1; h /= 2, o /= 2) r += lane & o ? h : 0;
   return r;
 }
-__device__ __forceinline__ bool any_of_256(bool v) {
+__device__ __forceinline__ bool any_of(bool v, int barrier, int threads) {
   int r;
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, 1, 256, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, %2, %3, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
       : "=r"(r)
-      : "r"((int)v)
+      : "r"((int)v), "r"(barrier), "r"(threads)
       : "memory");
   return r != 0;
+}
+// two binary32 operations in one instruction
+__device__ __forceinline__ void mul2(float& a, float& b, float c) {
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "+f"(a), "+f"(b)
+      : "f"(c));
+}
+__device__ __forceinline__ void fma2(float& a, float& b, float m0, float m1, float c0, float c1) {  // a = a * m0 + c0, b = b * m1 + c1
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmov.b64 z, {%4, %5};\n\t"
+      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "+f"(a), "+f"(b)
+      : "f"(m0), "f"(m1), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ void add2(float& a, float& b, float c, float d) {
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "+f"(a), "+f"(b)
+      : "f"(c), "f"(d));
 }
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
@@ -88,6 +129,34 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]),
                "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
                : "memory");
+}
+__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+      "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+      "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+      "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// D[tmem] (+)= A[tmem] * B[smem desc], f16: a column of A holds two consecutive k of its lane's row
+__device__ __forceinline__ void mma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc,
+                                           uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      ".reg .b64 db;\n\tmov.b64 db, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(desc_hi)
+      : "memory");
 }
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ptx::smem_u32(dst)), "l"(src),
@@ -120,37 +189,40 @@ template <int D>
 __device__ __forceinline__ uint32_t q_byte(int r, int d) {
   return D == 128 ? r * 128 + (((d >> 4) ^ (r & 7)) << 4) + (d & 15) : r * 64 + (((d >> 4) ^ ((r >> 1) & 3)) << 4) + (d & 15);
 }
-// upper half of a shared-memory matrix descriptor: stride between groups of 8 rows (bytes), layout type
-__device__ __forceinline__ uint64_t desc_of(uint32_t addr, uint32_t lead, uint32_t stride, uint32_t layout) {
-  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | (uint64_t)1 << 46 |
-         (uint64_t)layout << 61;
-}
-constexpr uint32_t kSw128 = 2, kSw64 = 4, kSw32 = 6, kSwNone = 0;
+// Halves of a shared-memory matrix descriptor (K-major, swizzled): address and leading offset | stride between groups of
+// 8 rows, version, layout.  A step along K or to another tile is an addition to the lower half.
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr) { return ((addr & 0x3FFFFu) >> 4) | (1u << 16); }
+__host__ __device__ constexpr uint32_t desc_hi(uint32_t stride, uint32_t layout) { return (stride >> 4) | (1u << 14) | (layout << 29); }
+constexpr uint32_t kSw128 = 2, kSw64 = 4, kSw32 = 6;
 
 template <int D, int R>
 struct Cfg {
   static constexpr int kCtas = R <= 32 ? 2 : 1;  // per SM
+  // groups of 4 softmax warps, each with its share of the rows: 16 or 20 warps per SM, since a warp alone issues an
+  // instruction every eight cycles only
+  static constexpr int kGroups = R <= 32 ? 2 : 4;
+  static constexpr int kThreads = 32 * (4 * kGroups + 2);  // + loader, MMA issuer
   static constexpr int kTile = kKeys * D;        // bytes of a K or V tile
-  static constexpr int kKStages = D == 128 && R <= 32 ? 2 : 3;
-  static constexpr int kVStages = D == 128 && R <= 32 ? 1 : 2;
-  static constexpr int kP = R * kKeys * 2;       // bytes of P and of the widened V tile, two blocks of 64 keys each
-  static constexpr int kV16 = D * kKeys * 2;
+  static constexpr int kKStages = 3, kVStages = R <= 32 && D == 128 ? 2 : 3;
+  // P^T is kept [key][row] (rows contiguous: a thread stores its key's rows by 16 bytes): blocks of up to 64 rows, a key's
+  // row in the swizzle of its length
+  static constexpr int kPRow = R >= 64 ? 128 : 2 * R, kPBlock = kKeys * kPRow, kP = R * kKeys * 2;
   static constexpr int kQ = R * D;
-  static constexpr int kTmem = R == 128 ? 512 : 4 * R;  // S x 2, O
-  // byte offsets (O has 128 lanes: with D = 64 the upper ones come from what lies behind the V tile, and are not used)
-  static constexpr int oK = 0, oV = kKStages * kTile, oV16 = oV + kVStages * kTile, oP = oV16 + kV16, oQ = oP + kP, oCtl = oQ + 3 * kQ;
-  static_assert(D == 128 || kP + 3 * kQ + 2048 >= kV16 / 2, "reads behind the V tile stay in the buffer");
+  static constexpr int kO = 2 * R, kV16 = 3 * R;                           // columns: S x 2, O, the widened V tile (64)
+  static constexpr int kTmem = R == 128 ? 512 : R == 64 ? 256 : R == 32 ? 256 : 128;
+  // byte offsets
+  static constexpr int oK = 0, oV = kKStages * kTile, oP = oV + kVStages * kTile, oQ = oP + kP, oCtl = oQ + 3 * kQ;
 };
 
 template <int R>
 struct Ctl {
-  uint64_t k_full[3], k_empty[3], v_full[2], v_empty[2];
+  uint64_t k_full[3], k_empty[3], v_full[3], v_empty[3];
   uint64_t s_full[2], s_empty[2], p_full, o_full, q_full, drain;
-  alignas(16) float2 rcm[R];    // row's factor from raw scores to powers of two | its reference m
+  alignas(16) float rcm[R / 2][4];  // per two rows: factors from raw scores to powers of two | minus the references m
   float fac_l[R], fac_o[R];
   float wmax[4][R], lsum[4][R];
-  float ks[2][8], vs[2][8];     // by V stage: scales of a tile's 16-key pieces
-  int pid[2][8];                // and their pages
+  alignas(16) float ks[3][8], vs[3][8];  // by V stage: scales of a tile's 16-key pieces
+  alignas(16) int pid[3][8];             // and their pages
   uint32_t vis[2][R][4];        // by tile parity: draft of the tile sees key (bits)
   uint32_t nan_row[R][4];       // row's output is NaN in these dimensions
   int low[R], top[R];           // by draft of the tile: context keys > low are seen; a chain sees keys <= top
@@ -180,11 +252,18 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile in
   }
 }
 
+// The same for a whole warp: one lane looks.
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int32_t* status, int lane) {
+  int r = 1;
+  if (lane == 0) r = wait(bar, parity, abort_flag, status);
+  return __shfl_sync(0xffffffffu, r, 0) != 0;
+}
+
 template <int D, int R>
-__global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(const Args a, const __grid_constant__ CUtensorMap tm_k,
+__global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_kernel(const Args a, const __grid_constant__ CUtensorMap tm_k,
                                                                             const __grid_constant__ CUtensorMap tm_v) {
   using C = Cfg<D, R>;
-  constexpr int KS = C::kKStages, VS = C::kVStages, RH = R / 2;
+  constexpr int KS = C::kKStages, VS = C::kVStages, G = C::kGroups, RH = R / G, NS = 128 * G;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   Ctl<R>& S = *reinterpret_cast<Ctl<R>*>(smem + C::oCtl);
@@ -196,13 +275,13 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
     }
     for (int i = 0; i < VS; ++i) {
       ptx::mbar_init(&S.v_full[i], 1);
-      ptx::mbar_init(&S.v_empty[i], 8);
+      ptx::mbar_init(&S.v_empty[i], 4 * G);
     }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&S.s_full[i], 1);
-      ptx::mbar_init(&S.s_empty[i], 8);
+      ptx::mbar_init(&S.s_empty[i], 4 * G);
     }
-    ptx::mbar_init(&S.p_full, 8);
+    ptx::mbar_init(&S.p_full, 4 * G);
     ptx::mbar_init(&S.o_full, 1);
     ptx::mbar_init(&S.q_full, 1);
     ptx::mbar_init(&S.drain, 1);
@@ -213,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
   asm volatile("griddepcontrol.wait;" ::: "memory");
   // Tensor memory is taken behind the wait and dependents are released behind that: no kernel holds tensor memory while
   // it waits for one that still has to take it.
-  if (warp == 9) {
+  if (warp == 4 * G + 1) {
     ptx::tmem_alloc(&S.tmem, C::kTmem);
     ptx::tmem_relinquish();
   }
@@ -240,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
     const int low_max = a.window > 0 ? s.ctx + s.n - 1 - a.window : -1;
     const int words = tree ? (a.d.max_drafts + 31) >> 5 : 0;
 
-    if (warp == 8) {
+    if (warp == 4 * G) {
       // ------------------------------------------------------------ loader
       asm volatile("fence.proxy.async;" ::: "memory");  // the cache was written by ordinary stores of earlier kernels
       if (lane == 0) {
@@ -252,14 +331,24 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
         const int key = k_begin + it * kKeys + 16 * seg;
         return it < n_tiles && key < k_all ? kv::page_of(a.d, a.c, b, key >> page_log2) : -1;
       };
-      int pid = page_at(0);
+      // page ids two tiles ahead, scales one: each is a trip to memory that the copies do not wait for
+      auto scale_at = [&](int p, float& k, float& v) {
+        const long long slot = (long long)max(p, 0) * a.c.heads + head;
+        k = p >= 0 ? __ldg(a.c.ks + slot) : 0.f;
+        v = p >= 0 ? __ldg(a.c.vs + slot) : 0.f;
+      };
+      int pid = page_at(0), pid1 = page_at(1);
+      float ks, vs;
+      scale_at(pid, ks, vs);
       for (int it = 0; it < n_tiles; ++it) {
         const int sk = it % KS, sv = it % VS;
-        const int next = page_at(it + 1);
+        const int pid2 = page_at(it + 2);
+        float ks1, vs1;
+        scale_at(pid1, ks1, vs1);
         const int mine = __shfl_sync(0xffffffffu, pid, ((lane & 7) << page_log2) >> 4 & 7);  // page `lane` of the tile
         const bool on = lane < pages && mine >= 0;
         const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, on)) * page * D;
-        if (it >= KS && __any_sync(0xffffffffu, !wait(&S.k_empty[sk], ((it / KS) & 1) ^ 1, &S.abort, a.d.status))) break;
+        if (it >= KS && !wait_warp(&S.k_empty[sk], ((it / KS) & 1) ^ 1, &S.abort, a.d.status, lane)) break;
         uint8_t* dst = smem + C::oK + sk * C::kTile + (lane & 7) * page * D;
         if (lane == 0) {
           ptx::mbar_arrive_expect_tx(&S.k_full[sk], bytes);
@@ -267,11 +356,10 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
         }
         __syncwarp();
         if (on) ptx::tma_load_2d(dst, &tm_k, &S.k_full[sk], 0, (mine * a.c.heads + head) << page_log2, ptx::kPolicyEvictNormal);
-        if (it >= VS && __any_sync(0xffffffffu, !wait(&S.v_empty[sv], ((it / VS) & 1) ^ 1, &S.abort, a.d.status))) break;
+        if (it >= VS && !wait_warp(&S.v_empty[sv], ((it / VS) & 1) ^ 1, &S.abort, a.d.status, lane)) break;
         if (lane < 8) {
-          const long long slot = (long long)max(pid, 0) * a.c.heads + head;
-          S.ks[sv][lane] = pid >= 0 ? a.c.ks[slot] : 0.f;
-          S.vs[sv][lane] = pid >= 0 ? a.c.vs[slot] : 0.f;
+          S.ks[sv][lane] = ks;
+          S.vs[sv][lane] = vs;
           S.pid[sv][lane] = pid;
         }
         __syncwarp();
@@ -285,15 +373,19 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
           if (page_log2 == 4) bulk_load(dst, a.c.v + ((long long)mine * a.c.heads + head) * (D * 16), D * 16, &S.v_full[sv]);
           else ptx::tma_load_2d(dst, &tm_v, &S.v_full[sv], 0, (mine * a.c.heads + head) * D, ptx::kPolicyEvictNormal);
         }
-        pid = next;
+        pid = pid1;
+        pid1 = pid2;
+        ks = ks1;
+        vs = vs1;
       }
-    } else if (warp == 9) {
+    } else if (warp == 4 * G + 1) {
       // ------------------------------------------------------------ MMA issuer
       if (lane == 0) {
         const uint32_t idesc = ptx::instr_desc(0, 0, R);  // e4m3 x e4m3 in kind::f8f6f4, f16 x f16 in kind::f16
-        const uint32_t kb = ptx::smem_u32(smem + C::oK), vb = ptx::smem_u32(smem + C::oV16), pb = ptx::smem_u32(smem + C::oP),
-                       qb = ptx::smem_u32(smem + C::oQ);
-        constexpr uint32_t kLay = D == 128 ? kSw128 : kSw64;
+        const uint32_t pdesc = idesc | (1u << 16);  // B with its rows (N) contiguous
+        // leading offset of P: from one block of 64 rows to the next
+        const uint32_t kb = desc_lo(ptx::smem_u32(smem + C::oK)), pb = (desc_lo(ptx::smem_u32(smem + C::oP)) & 0xFFFFu) | (uint32_t)(C::kPBlock / 16) << 16, qb = desc_lo(ptx::smem_u32(smem + C::oQ));
+        constexpr uint32_t kHi = desc_hi(8 * D, D == 128 ? kSw128 : kSw64), pHi = desc_hi(8 * C::kPRow, C::kPRow == 128 ? kSw128 : C::kPRow == 64 ? kSw64 : kSw32);
         bool ok = true;
         auto scores = [&](int it) {
           const int st = it % KS, u = it & 1;
@@ -301,12 +393,12 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
           if (it >= 2) ok = ok && wait(&S.s_empty[u], ((it >> 1) & 1) ^ 1, &S.abort, a.d.status);
           if (!ok) return;
           ptx::tc_fence_after();
+          const uint32_t ka = kb + st * (C::kTile / 16);
 #pragma unroll
           for (int term = 0; term < 3; ++term)
 #pragma unroll
             for (int k = 0; k < D / 32; ++k)
-              ptx::mma_f8f6f4(tmem + u * R, desc_of(kb + st * C::kTile + k * 32, 16, 8 * D, kLay),
-                              desc_of(qb + term * C::kQ + k * 32, 16, 8 * D, kLay), idesc, term + k > 0);
+              ptx::mma_f8f6f4_lohi(tmem + u * R, ka + k * 2, qb + (term * C::kQ + k * 32) / 16, kHi, idesc, term + k > 0);
           ptx::mma_commit(&S.k_empty[st]);
           ptx::mma_commit(&S.s_full[u]);
         };
@@ -321,8 +413,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
           ptx::tc_fence_after();
 #pragma unroll
           for (int k = 0; k < kKeys / 16; ++k)
-            ptx::mma_f16(tmem + 2 * R, desc_of(vb + (k >> 2) * (C::kV16 / 2) + (k & 3) * 32, 16, 1024, kSw128),
-                         desc_of(pb + (k >> 2) * (C::kP / 2) + (k & 3) * 32, 16, 1024, kSw128), idesc, it + k > 0);
+            mma_f16_ta(tmem + C::kO, tmem + C::kV16 + k * 8, pb + k * C::kPRow, pHi, pdesc, it + k > 0);  // 16 keys on
           ptx::mma_commit(&S.o_full);
         }
         if (!ok) {  // abort: what was issued must have ended before tensor memory and shared memory are given back
@@ -331,13 +422,13 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
       }
     } else {
       // ------------------------------------------------------------ softmax
-      const int quad = warp & 3, half = warp >> 2, r0 = half * RH, key = quad * 32 + lane;
+      const int quad = warp & 3, group = warp >> 2, r0 = group * RH, key = quad * 32 + lane;
       uint32_t* anc = reinterpret_cast<uint32_t*>(smem + C::oCtl + sizeof(Ctl<R>));  // [R][words]
       int* par = reinterpret_cast<int*>(anc + R * words);
       if (tree) {
-        for (int i = tid; i < s.n; i += 256) par[i] = kv::parent_of(a.d.parent + s.lo, i);
-        for (int i = tid; i < R * words; i += 256) anc[i] = 0;
-        ptx::named_barrier(2, 256);
+        for (int i = tid; i < s.n; i += NS) par[i] = kv::parent_of(a.d.parent + s.lo, i);
+        for (int i = tid; i < R * words; i += NS) anc[i] = 0;
+        ptx::named_barrier(2, NS);
       }
       if (tid <= i_last - i_first) {  // one thread per draft of the tile
         const int i = i_first + tid;
@@ -351,10 +442,10 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
         S.low[tid] = a.window > 0 ? at - a.window : -1;
         S.top[tid] = tree ? s.ctx - 1 : at;
       }
-      for (int i = tid; i < R * 4; i += 256) (&S.nan_row[0][0])[i] = 0;
+      for (int i = tid; i < R * 4; i += NS) (&S.nan_row[0][0])[i] = 0;
       // Q: a row's D elements by D / 8 neighbouring lanes, 8 each
       constexpr int kPer = D / 8;
-      for (int z = tid; z < R * kPer; z += 256) {
+      for (int z = tid; z < R * kPer; z += NS) {
         const int r = z / kPer, d0 = (z % kPer) * 8, rr = row0 + r;
         const bool live = rr < n_rows;
         const int i = rr / a.rep, hq = head * a.rep + rr % a.rep;
@@ -374,7 +465,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
           back = ldexpf(1.f, ex - 7);
         }
         if ((z % kPer) == 0) {
-          S.rcm[r] = make_float2(a.scale_log2 * back, kUnseen);
+          S.rcm[r / 2][r & 1] = a.scale_log2 * back;
+          S.rcm[r / 2][2 + (r & 1)] = -kUnseen;
           S.row[r] = live ? make_int2(s.lo + i, hq) : make_int2(-1, 0);
         }
         uint32_t code[3][2] = {};
@@ -395,7 +487,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
           *reinterpret_cast<uint2*>(smem + C::oQ + term * C::kQ + q_byte<D>(r, d0)) = make_uint2(code[term][0], code[term][1]);
       }
       ptx::fence_proxy_async_smem();
-      ptx::named_barrier(2, 256);
+      ptx::named_barrier(2, NS);
       if (tid == 0) ptx::mbar_arrive(&S.q_full);
 
       float l[RH];
@@ -403,17 +495,18 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
       for (int r = 0; r < RH; ++r) l[r] = 0.f;
       float u = 0.f;  // V scale that the accumulators are in units of
       const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-      uint32_t xo[8];  // this key's place in row r of P: (r & 7) selects
-#pragma unroll
-      for (int k = 0; k < 8; ++k) xo[k] = (key >> 6) * (C::kP / 2) + ((((key & 63) >> 3) ^ k) << 4) + (key & 7) * 2 + r0 * 128;
+      // this key's row of P; 16-byte piece c of it is at c ^ p_xor
+      uint8_t* const p_row = smem + C::oP + (r0 / 64) * C::kPBlock + key * C::kPRow;
+      const int p_xor = C::kPRow == 128 ? key & 7 : C::kPRow == 64 ? (key >> 1) & 3 : (key >> 2) & 1;
       bool ok = true;
       for (int it = 0; it < n_tiles; ++it) {
         const int sv = it % VS, bu = it & 1;
         const int k0 = k_begin + it * kKeys;
         const bool masked = k0 + kKeys > s.ctx || k0 <= low_max;  // somebody may not see a key of the tile
         if (masked) {
-          // what each draft of the tile sees of its keys
-          for (int z = tid; z < (i_last - i_first + 1) * 4; z += 256) {
+          // what each draft of the tile sees of its keys.  Every group writes all of it (the same words), so that nobody waits
+          // for another group here
+          for (int z = quad * 32 + lane; z < (i_last - i_first + 1) * 4; z += 128) {
             const int dr = z >> 2, kb = k0 + (z & 3) * 32;
             const int from = max(0, S.low[dr] + 1 - kb), to = min(32, S.top[dr] + 1 - kb);
             uint32_t bits = to > from ? (0xffffffffu >> (32 - to)) & (0xffffffffu << from) : 0u;
@@ -425,23 +518,28 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
             }
             S.vis[bu][dr][z & 3] = bits;
           }
-          ptx::named_barrier(2, 256);
+          ptx::named_barrier(3 + group, 128);
         }
-        ok = wait(&S.v_full[sv], (it / VS) & 1, &S.abort, a.d.status) && ok;
-        ok = wait(&S.s_full[bu], (it >> 1) & 1, &S.abort, a.d.status) && ok;
+        ok = wait_warp(&S.v_full[sv], (it / VS) & 1, &S.abort, a.d.status, lane) && ok;
+        ok = wait_warp(&S.s_full[bu], (it >> 1) & 1, &S.abort, a.d.status, lane) && ok;
         ptx::tc_fence_after();
         const float k_scale = S.ks[sv][key >> 4], v_scale = S.vs[sv][key >> 4];
         const bool there = S.pid[sv][key >> 4] >= 0;
         float vm = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) vm = fmaxf(vm, S.vs[sv][e]);
+        bool plain = !masked;  // every key is there and every row sees it
+        {
+          const float4 x = *reinterpret_cast<const float4*>(&S.vs[sv][0]), y = *reinterpret_cast<const float4*>(&S.vs[sv][4]);
+          vm = fmaxf(fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)), fmaxf(fmaxf(y.x, y.y), fmaxf(y.z, y.w)));
+          const int4 i = *reinterpret_cast<const int4*>(&S.pid[sv][0]), j = *reinterpret_cast<const int4*>(&S.pid[sv][4]);
+          plain = plain && (i.x | i.y | i.z | i.w | j.x | j.y | j.z | j.w) >= 0;
+        }
         float v[RH];
         auto load_scores = [&]() {  // times the page's scale; -inf where the row does not see this thread's key
 #pragma unroll
           for (int c = 0; c < RH / 8; ++c) tmem_ld8(tmem + lane_base + bu * R + r0 + 8 * c, *reinterpret_cast<uint32_t(*)[8]>(&v[8 * c]));
           ptx::tmem_ld_wait();
 #pragma unroll
-          for (int r = 0; r < RH; ++r) v[r] *= k_scale;
+          for (int r = 0; r < RH; r += 2) mul2(v[r], v[r + 1], k_scale);
           if (masked) {
             int dr = (row0 + r0) / a.rep, in = row0 + r0 - dr * a.rep;  // row's draft and its head
             dr -= i_first;
@@ -465,58 +563,55 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
         float tmax = ok ? -INFINITY : INFINITY;
 #pragma unroll
         for (int r = 0; r < RH; r += 2) {
-          const float4 q = *reinterpret_cast<const float4*>(&S.rcm[r0 + r]);
-          v[r] = fmaf(v[r], q.x, -q.y);
-          v[r + 1] = fmaf(v[r + 1], q.z, -q.w);
+          const float4 q = *reinterpret_cast<const float4*>(&S.rcm[(r0 + r) / 2][0]);
+          fma2(v[r], v[r + 1], q.x, q.y, q.z, q.w);
           tmax = fmaxf(tmax, fmaxf(v[r], v[r + 1]));
         }
-        const bool unit = vm > 0.f && (vm > u || vm < u * (1.f / 64.f));  // the same in every thread
-        if (any_of_256(tmax > kLimit || unit)) {
-          if (any_of_256(!ok)) {  // a thread that gave up stays with the others' barriers until here: all of them leave
+        const bool unit = vm > 0.f && (vm > u * kUnitUp || vm < u * kUnitDown);  // the same in the group's threads
+        if (any_of(tmax > kLimit || unit, 3 + group, 128)) {
+          if (any_of(!ok, 3 + group, 128)) {  // a warp that gave up stays with the others' barriers until here: all of them leave
             ok = false;
             break;
           }
           // move the references to the maxima and the unit to the tile's largest V scale.  From the scores themselves:
           // relative to the reference of a row that has seen nothing they have lost their digits
           load_scores();
+          float x[RH];
 #pragma unroll
-          for (int r = 0; r < RH; ++r) {
-            v[r] *= S.rcm[r0 + r].x;
-            const float m = warp_max(v[r]);
-            if (lane == 0) S.wmax[quad][r0 + r] = m;
-          }
-          ptx::named_barrier(2, 256);
+          for (int r = 0; r < RH; ++r) x[r] = v[r] = v[r] * S.rcm[(r0 + r) / 2][r & 1];
+          const float top = warp_reduce<RH, true>(x, lane);
+          S.wmax[quad][r0 + reduced_index<RH>(lane)] = top;
+          ptx::named_barrier(3 + group, 128);
           const float u_new = unit ? vm : u;
-          if (tid < R) {
-            const float old = S.rcm[tid].y;
-            const float m = fmaxf(fmaxf(old, fmaxf(S.wmax[0][tid], S.wmax[1][tid])), fmaxf(S.wmax[2][tid], S.wmax[3][tid]));
+          if (const int r = r0 + quad * 32 + lane; r < r0 + RH) {
+            const float old = -S.rcm[r / 2][2 + (r & 1)];
+            const float m = fmaxf(fmaxf(old, fmaxf(S.wmax[0][r], S.wmax[1][r])), fmaxf(S.wmax[2][r], S.wmax[3][r]));
             const float fl = exp2_fast(old - m);
-            S.rcm[tid].y = m;
-            S.fac_l[tid] = fl;
-            S.fac_o[tid] = fl * (u / u_new);
+            S.rcm[r / 2][2 + (r & 1)] = -m;
+            S.fac_l[r] = fl;
+            S.fac_o[r] = fl * (u / u_new);
           }
-          ptx::named_barrier(2, 256);
+          ptx::named_barrier(3 + group, 128);
           u = u_new;
 #pragma unroll
           for (int r = 0; r < RH; ++r) {
             l[r] *= S.fac_l[r0 + r];
-            v[r] -= S.rcm[r0 + r].y;
+            v[r] += S.rcm[(r0 + r) / 2][2 + (r & 1)];
           }
           if (it > 0) {
-            ok = wait(&S.o_full, (it - 1) & 1, &S.abort, a.d.status) && ok;  // the second product of tile it - 1 has ended
+            ok = wait_warp(&S.o_full, (it - 1) & 1, &S.abort, a.d.status, lane) && ok;  // the second product of tile it - 1 has ended
             ptx::tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < RH / 8; ++c) {
               uint32_t o[8];
-              const uint32_t at = tmem + lane_base + 2 * R + r0 + 8 * c;
+              const uint32_t at = tmem + lane_base + C::kO + r0 + 8 * c;
               tmem_ld8(at, o);
               ptx::tmem_ld_wait();
 #pragma unroll
               for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * S.fac_o[r0 + 8 * c + e]);
               tmem_st8(at, o);
             }
-            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-            ptx::tc_fence_before();
+            tmem_st_wait();
           }
         }
         ptx::tc_fence_before();
@@ -527,56 +622,52 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
 #pragma unroll
         for (int r = 0; r < RH; r += 2) {
           const float p0 = exp2_fast(v[r]), p1 = exp2_fast(v[r + 1]);
-          l[r] += p0;
-          l[r + 1] += p1;
+          add2(l[r], l[r + 1], p0, p1);
           const __half2 h = __hmul2(__floats2half2_rn(p0, p1), f);
           p[r / 2] = *reinterpret_cast<const uint32_t*>(&h);
         }
         // P and the widened V are free once the second product of the tile before has ended
-        if (it > 0) ok = wait(&S.o_full, (it - 1) & 1, &S.abort, a.d.status) && ok;
-        uint8_t* pt = smem + C::oP;
+        if (it > 0) ok = wait_warp(&S.o_full, (it - 1) & 1, &S.abort, a.d.status, lane) && ok;
 #pragma unroll
-        for (int r = 0; r < RH; r += 2) {
-          *reinterpret_cast<uint16_t*>(pt + r * 128 + xo[r & 7]) = (uint16_t)p[r / 2];
-          *reinterpret_cast<uint16_t*>(pt + (r + 1) * 128 + xo[(r + 1) & 7]) = (uint16_t)(p[r / 2] >> 16);
-        }
-        const uint8_t* vt = smem + C::oV + sv * C::kTile;
-        uint8_t* wt = smem + C::oV16;
+        for (int c = 0; c < RH / 8; ++c)
+          *reinterpret_cast<uint4*>(p_row + (((r0 % 64) / 8 + c) ^ p_xor) * 16) = make_uint4(p[4 * c], p[4 * c + 1], p[4 * c + 2], p[4 * c + 3]);
+        // V: this thread's dimension (its lane of tensor memory), its group's share of the keys
+        const int d = quad * 32 + lane;
+        if (quad * 32 < D) {
+          const uint8_t* vt = smem + C::oV + sv * C::kTile;
+          uint32_t w16[64 / G];
 #pragma unroll
-        for (int z0 = 0; z0 < D * 8; z0 += 256) {
-          const int z = z0 + tid, d = z >> 3, seg = z & 7;
-          const uint4 w = *reinterpret_cast<const uint4*>(vt + v_piece<D>(d, seg, page_log2));
-          uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-          if (masked || S.pid[sv][seg] < 0) {
-            // keys behind the end or without a page count as zero, so that 0 * V is 0; a NaN of a written key goes to the
-            // rows that see the key, and to no others
-            const int have = S.pid[sv][seg] < 0 ? 0 : min(16, max(0, k_all - (k0 + 16 * seg)));
+          for (int z = 0; z < 8 / G; ++z) {
+            const int seg = group * (8 / G) + z;
+            const uint4 w = *reinterpret_cast<const uint4*>(vt + v_piece<D>(d, seg, page_log2));
+            uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+            if (!plain) {
+              // keys behind the end or without a page count as zero, so that 0 * V is 0; a NaN of a written key goes to the
+              // rows that see the key, and to no others
+              const int have = S.pid[sv][seg] < 0 ? 0 : min(16, max(0, k_all - (k0 + 16 * seg)));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int keep = min(4, max(0, have - 4 * e));
-              if (keep < 4) ww[e] &= keep == 0 ? 0u : 0xffffffffu >> (32 - 8 * keep);
-              const uint32_t bad = __vcmpeq4(ww[e] & 0x7f7f7f7fu, 0x7f7f7f7fu);
-              if (masked && bad) {
-                ww[e] &= ~bad;
-                for (int y = 0; y < 4; ++y)
-                  if ((bad >> (8 * y)) & 1u) {
-                    const int kk = seg * 16 + 4 * e + y;
-                    for (int r = 0; r < R && row0 + r < n_rows; ++r)
-                      if ((S.vis[bu][(row0 + r) / a.rep - i_first][kk >> 5] >> (kk & 31)) & 1u) atomicOr(&S.nan_row[r][d >> 5], 1u << (d & 31));
-                  }
+              for (int e = 0; e < 4; ++e) {
+                const int keep = min(4, max(0, have - 4 * e));
+                if (keep < 4) ww[e] &= keep == 0 ? 0u : 0xffffffffu >> (32 - 8 * keep);
+                const uint32_t bad = __vcmpeq4(ww[e] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+                if (masked && bad) {
+                  ww[e] &= ~bad;
+                  for (int y = 0; y < 4; ++y)
+                    if ((bad >> (8 * y)) & 1u) {
+                      const int kk = seg * 16 + 4 * e + y;
+                      for (int r = 0; r < R && row0 + r < n_rows; ++r)
+                        if ((S.vis[bu][(row0 + r) / a.rep - i_first][kk >> 5] >> (kk & 31)) & 1u) atomicOr(&S.nan_row[r][d >> 5], 1u << (d & 31));
+                    }
+                }
               }
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) codes_to_f16(ww[e], w16[8 * z + 2 * e], w16[8 * z + 2 * e + 1]);
           }
-          uint4 x, y;
-          codes_to_f16(ww[0], x.x, x.y);
-          codes_to_f16(ww[1], x.z, x.w);
-          codes_to_f16(ww[2], y.x, y.y);
-          codes_to_f16(ww[3], y.z, y.w);
-          uint8_t* at = wt + (seg >> 2) * (C::kV16 / 2) + d * 128;
-          const int ch = (seg & 3) * 2;
-          *reinterpret_cast<uint4*>(at + ((ch ^ (d & 7)) << 4)) = x;
-          *reinterpret_cast<uint4*>(at + (((ch + 1) ^ (d & 7)) << 4)) = y;
+          tmem_st(tmem + lane_base + C::kV16 + group * (64 / G), w16);
+          tmem_st_wait();
         }
+        ptx::tc_fence_before();
         ptx::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
@@ -585,22 +676,17 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
         }
       }
       // ---- results
-      if (ok && n_tiles > 0) ok = wait(&S.o_full, (n_tiles - 1) & 1, &S.abort, a.d.status);
+      if (ok && n_tiles > 0) ok = wait_warp(&S.o_full, (n_tiles - 1) & 1, &S.abort, a.d.status, lane);
       ptx::tc_fence_after();
-#pragma unroll
-      for (int r = 0; r < RH; ++r) {
-        float x = l[r];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-        if (lane == 0) S.lsum[quad][r0 + r] = x;
-      }
-      if (!any_of_256(!ok)) {
+      const float sum = warp_reduce<RH, false>(l, lane);
+      S.lsum[quad][r0 + reduced_index<RH>(lane)] = sum;
+      if (!any_of(!ok, 3 + group, 128)) {
         const int d = quad * 32 + lane;
         const bool split = a.chunks > 1;
 #pragma unroll 1
         for (int c = 0; c < RH / 8; ++c) {
           uint32_t oh[8];
-          const uint32_t at = tmem + lane_base + 2 * R + r0 + 8 * c;
+          const uint32_t at = tmem + lane_base + C::kO + r0 + 8 * c;
           if (n_tiles > 0) {
             tmem_ld8(at, oh);
             ptx::tmem_ld_wait();
@@ -614,7 +700,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
             const int2 ro = S.row[r];
             if (ro.x < 0 || d >= D) continue;
             float den = (S.lsum[0][r] + S.lsum[1][r]) + (S.lsum[2][r] + S.lsum[3][r]);
-            float m = den == 0.f ? -INFINITY : S.rcm[r].y;
+            float m = den == 0.f ? -INFINITY : -S.rcm[r / 2][2 + (r & 1)];
             float o = __uint_as_float(oh[e]) * u;
             if ((S.nan_row[r][d >> 5] >> (d & 31)) & 1u) o = __int_as_float(0x7fffffff);
             if (split) {
@@ -636,7 +722,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
         }
       }
     }
-    if (S.abort && warp == 8 && lane == 0) {  // copies in flight land before the shared memory is given back
+    if (S.abort && warp == 4 * G && lane == 0) {  // copies in flight land before the shared memory is given back
       ptx::drain_ring(S.k_full, KS, S.k_it, kBudgetNs);
       ptx::drain_ring(S.v_full, VS, S.v_it, kBudgetNs);
     }
@@ -644,7 +730,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, R>::kCtas) attend_kernel(cons
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
-  if (warp == 9) ptx::tmem_dealloc(tmem, C::kTmem);
+  if (warp == 4 * G + 1) ptx::tmem_dealloc(tmem, C::kTmem);
 }
 
 // One warp per (token, head): the chunks' parts, in order, and the sink.

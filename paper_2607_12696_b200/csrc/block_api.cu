@@ -210,7 +210,7 @@ bool encode_rows(CUtensorMap* m, const void* ptr, int width, long long rows, int
 template <int D, int R>
 cudaError_t launch_attend(const att::Args& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
   const size_t smem = att::smem_bytes<D, R>((a.d.max_drafts + 31) / 32, a.d.parent != nullptr);
-  return launch(att::attend_kernel<D, R>, dim3(a.chunks, a.c.heads * a.row_tiles, a.d.n_seq), dim3(att::kThreads), smem, st, a, tk, tv);
+  return launch(att::attend_kernel<D, R>, dim3(a.chunks, a.c.heads * a.row_tiles, a.d.n_seq), dim3(att::Cfg<D, R>::kThreads), smem, st, a, tk, tv);
 }
 template <int D>
 cudaError_t launch_attend_d(const att::Args& a, int rows, cudaStream_t st) {
