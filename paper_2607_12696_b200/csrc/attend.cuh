@@ -11,7 +11,8 @@
 // K codes go from the cache by TMA to shared memory and from there to the multiplier as they are (a tile is 128 / page
 // pages side by side); kind::f8f6f4 wants 8-bit operands on both sides, so q (bf16) is three e4m3 terms of q * 2^e, its
 // largest element in [128, 256): each term takes the rest of the one before, what is left is 2^-18 of the row's largest
-// element or 2^-12 of the element, whichever is more.  They add in one accumulator.
+// element or 2^-12 of the element, whichever is more.  Up to R = 64 the terms stand side by side as 3 R columns, added as
+// they are read: an instruction takes about 75 cycles however narrow it is; at R = 128 they add in one accumulator.
 // The second product runs in kind::f16: V codes, exact in f16, are widened on their way into tensor memory, which
 // holds the A operand (16 KB of codes per tile, whatever R), and p is rounded once to f16 (2^-11).  In 8 bits p would need
 // two terms and leave the reference below 3 bits of room.
@@ -203,15 +204,20 @@ struct Cfg {
   static constexpr int kGroups = R <= 32 ? 2 : 4;
   static constexpr int kThreads = 32 * (4 * kGroups + 2);  // + loader, MMA issuer
   static constexpr int kTile = kKeys * D;        // bytes of a K or V tile
-  static constexpr int kKStages = 3, kVStages = R <= 32 && D == 128 ? 2 : 3;
+  static constexpr int kKStages = R <= 32 && D == 128 ? 2 : 3, kVStages = 3;
+  // scores: columns of a tile, buffers (where two CTAs share the SM, the other one's work covers for the second)
+  static constexpr int kSCols = R <= 64 ? 3 * R : R, kSBufs = R <= 32 ? 1 : 2;
+  static constexpr int kPBufs = R == 128 ? 2 : 1;
+  static constexpr int kChunk = R / kGroups < 16 ? R / kGroups : 16;  // rows that a thread works on at a time
   // P^T is kept [key][row] (rows contiguous: a thread stores its key's rows by 16 bytes): blocks of up to 64 rows, a key's
   // row in the swizzle of its length
   static constexpr int kPRow = R >= 64 ? 128 : 2 * R, kPBlock = kKeys * kPRow, kP = R * kKeys * 2;
   static constexpr int kQ = R * D;
-  static constexpr int kO = 2 * R, kV16 = 3 * R;                           // columns: S x 2, O, the widened V tile (64)
-  static constexpr int kTmem = R == 128 ? 512 : R == 64 ? 256 : R == 32 ? 256 : 128;
+  static constexpr int kO = kSBufs * kSCols, kV16 = kO + R;  // columns: S, O, the widened V tile (64)
+  static constexpr int kTmem = R == 16 ? 128 : R == 32 ? 256 : 512;
+  static_assert(kV16 + 64 <= kTmem, "tensor memory");
   // byte offsets
-  static constexpr int oK = 0, oV = kKStages * kTile, oP = oV + kVStages * kTile, oQ = oP + kP, oCtl = oQ + 3 * kQ;
+  static constexpr int oK = 0, oV = kKStages * kTile, oP = oV + kVStages * kTile, oQ = oP + kPBufs * kP, oCtl = oQ + 3 * kQ;
 };
 
 template <int R>
@@ -263,7 +269,7 @@ template <int D, int R>
 __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_kernel(const Args a, const __grid_constant__ CUtensorMap tm_k,
                                                                             const __grid_constant__ CUtensorMap tm_v) {
   using C = Cfg<D, R>;
-  constexpr int KS = C::kKStages, VS = C::kVStages, G = C::kGroups, RH = R / G, NS = 128 * G;
+  constexpr int KS = C::kKStages, VS = C::kVStages, SB = C::kSBufs, G = C::kGroups, RH = R / G, RC = C::kChunk, NS = 128 * G;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   Ctl<R>& S = *reinterpret_cast<Ctl<R>*>(smem + C::oCtl);
@@ -381,24 +387,24 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
     } else if (warp == 4 * G + 1) {
       // ------------------------------------------------------------ MMA issuer
       if (lane == 0) {
-        const uint32_t idesc = ptx::instr_desc(0, 0, R);  // e4m3 x e4m3 in kind::f8f6f4, f16 x f16 in kind::f16
-        const uint32_t pdesc = idesc | (1u << 16);  // B with its rows (N) contiguous
+        const uint32_t sdesc = ptx::instr_desc(0, 0, C::kSCols);        // kind::f8f6f4: e4m3 x e4m3
+        const uint32_t pdesc = ptx::instr_desc(0, 0, R) | (1u << 16);  // kind::f16: f16 x f16, B with its rows (N) contiguous
         // leading offset of P: from one block of 64 rows to the next
         const uint32_t kb = desc_lo(ptx::smem_u32(smem + C::oK)), pb = (desc_lo(ptx::smem_u32(smem + C::oP)) & 0xFFFFu) | (uint32_t)(C::kPBlock / 16) << 16, qb = desc_lo(ptx::smem_u32(smem + C::oQ));
         constexpr uint32_t kHi = desc_hi(8 * D, D == 128 ? kSw128 : kSw64), pHi = desc_hi(8 * C::kPRow, C::kPRow == 128 ? kSw128 : C::kPRow == 64 ? kSw64 : kSw32);
         bool ok = true;
         auto scores = [&](int it) {
-          const int st = it % KS, u = it & 1;
+          const int st = it % KS, u = it % SB;
           ok = ok && wait(&S.k_full[st], (it / KS) & 1, &S.abort, a.d.status);
-          if (it >= 2) ok = ok && wait(&S.s_empty[u], ((it >> 1) & 1) ^ 1, &S.abort, a.d.status);
+          if (it >= SB) ok = ok && wait(&S.s_empty[u], ((it / SB) & 1) ^ 1, &S.abort, a.d.status);
           if (!ok) return;
           ptx::tc_fence_after();
           const uint32_t ka = kb + st * (C::kTile / 16);
 #pragma unroll
-          for (int term = 0; term < 3; ++term)
+          for (int term = 0; term < (C::kSCols == R ? 3 : 1); ++term)
 #pragma unroll
             for (int k = 0; k < D / 32; ++k)
-              ptx::mma_f8f6f4_lohi(tmem + u * R, ka + k * 2, qb + (term * C::kQ + k * 32) / 16, kHi, idesc, term + k > 0);
+              ptx::mma_f8f6f4_lohi(tmem + u * C::kSCols, ka + k * 2, qb + (term * C::kQ + k * 32) / 16, kHi, sdesc, term + k > 0);
           ptx::mma_commit(&S.k_empty[st]);
           ptx::mma_commit(&S.s_full[u]);
         };
@@ -413,7 +419,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
           ptx::tc_fence_after();
 #pragma unroll
           for (int k = 0; k < kKeys / 16; ++k)
-            mma_f16_ta(tmem + C::kO, tmem + C::kV16 + k * 8, pb + k * C::kPRow, pHi, pdesc, it + k > 0);  // 16 keys on
+            mma_f16_ta(tmem + C::kO, tmem + C::kV16 + k * 8, pb + (it % C::kPBufs) * (C::kP / 16) + k * C::kPRow, pHi, pdesc, it + k > 0);  // 16 keys on
           ptx::mma_commit(&S.o_full);
         }
         if (!ok) {  // abort: what was issued must have ended before tensor memory and shared memory are given back
@@ -493,11 +499,16 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
       float l[RH];
 #pragma unroll
       for (int r = 0; r < RH; ++r) l[r] = 0.f;
-      float u = 0.f;  // V scale that the accumulators are in units of
+      float unit_of[RH / RC];  // V scale that the accumulators of each part of the rows are in units of
+#pragma unroll
+      for (int c = 0; c < RH / RC; ++c) unit_of[c] = 0.f;
       const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
       // this key's row of P; 16-byte piece c of it is at c ^ p_xor
-      uint8_t* const p_row = smem + C::oP + (r0 / 64) * C::kPBlock + key * C::kPRow;
+      uint8_t* const p_row0 = smem + C::oP + (r0 / 64) * C::kPBlock + key * C::kPRow;
       const int p_xor = C::kPRow == 128 ? key & 7 : C::kPRow == 64 ? (key >> 1) & 3 : (key >> 2) & 1;
+      uint32_t v_off[8 / G];
+#pragma unroll
+      for (int z = 0; z < 8 / G; ++z) v_off[z] = v_piece<D>(quad * 32 + lane, group * (8 / G) + z, page_log2);
       bool ok = true;
       for (int it = 0; it < n_tiles; ++it) {
         const int sv = it % VS, bu = it & 1;
@@ -521,11 +532,11 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
           ptx::named_barrier(3 + group, 128);
         }
         ok = wait_warp(&S.v_full[sv], (it / VS) & 1, &S.abort, a.d.status, lane) && ok;
-        ok = wait_warp(&S.s_full[bu], (it >> 1) & 1, &S.abort, a.d.status, lane) && ok;
+        ok = wait_warp(&S.s_full[it % SB], (it / SB) & 1, &S.abort, a.d.status, lane) && ok;
         ptx::tc_fence_after();
         const float k_scale = S.ks[sv][key >> 4], v_scale = S.vs[sv][key >> 4];
         const bool there = S.pid[sv][key >> 4] >= 0;
-        float vm = 0.f;
+        float vm;
         bool plain = !masked;  // every key is there and every row sees it
         {
           const float4 x = *reinterpret_cast<const float4*>(&S.vs[sv][0]), y = *reinterpret_cast<const float4*>(&S.vs[sv][4]);
@@ -533,104 +544,127 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
           const int4 i = *reinterpret_cast<const int4*>(&S.pid[sv][0]), j = *reinterpret_cast<const int4*>(&S.pid[sv][4]);
           plain = plain && (i.x | i.y | i.z | i.w | j.x | j.y | j.z | j.w) >= 0;
         }
-        float v[RH];
-        auto load_scores = [&]() {  // times the page's scale; -inf where the row does not see this thread's key
+        const uint32_t s_at = tmem + lane_base + (it % SB) * C::kSCols + r0;
+        uint8_t* const p_row = p_row0 + (it % C::kPBufs) * C::kP;
+        bool leave = false;
 #pragma unroll
-          for (int c = 0; c < RH / 8; ++c) tmem_ld8(tmem + lane_base + bu * R + r0 + 8 * c, *reinterpret_cast<uint32_t(*)[8]>(&v[8 * c]));
-          ptx::tmem_ld_wait();
+        for (int rc = 0; rc < RH; rc += RC) {  // RC of this thread's rows at a time
+          float v[RC];
+          auto load_scores = [&]() {  // times the page's scale; -inf where the row does not see this thread's key
+            float w[RC];
 #pragma unroll
-          for (int r = 0; r < RH; r += 2) mul2(v[r], v[r + 1], k_scale);
-          if (masked) {
-            int dr = (row0 + r0) / a.rep, in = row0 + r0 - dr * a.rep;  // row's draft and its head
-            dr -= i_first;
-            uint32_t bits = S.vis[bu][min(dr, i_last - i_first)][quad];
+            for (int term = 0; term < C::kSCols / R; ++term) {
+              float* const to = term ? w : v;
 #pragma unroll
-            for (int r = 0; r < RH; ++r) {
-              if (!((bits >> lane) & 1u)) v[r] = -INFINITY;
-              if (++in == a.rep) {
-                in = 0;
-                ++dr;
-                bits = S.vis[bu][min(dr, i_last - i_first)][quad];
+              for (int c = 0; c < RC / 8; ++c) tmem_ld8(s_at + term * R + rc + 8 * c, *reinterpret_cast<uint32_t(*)[8]>(to + 8 * c));
+              ptx::tmem_ld_wait();
+              if (term) {
+#pragma unroll
+                for (int r = 0; r < RC; r += 2) add2(v[r], v[r + 1], w[r], w[r + 1]);
               }
             }
-          }
-          if (!there) {
 #pragma unroll
-            for (int r = 0; r < RH; ++r) v[r] = -INFINITY;
-          }
-        };
-        load_scores();
-        float tmax = ok ? -INFINITY : INFINITY;
+            for (int r = 0; r < RC; r += 2) mul2(v[r], v[r + 1], k_scale);
+            if (masked) {
+              int dr = (row0 + r0 + rc) / a.rep, in = row0 + r0 + rc - dr * a.rep;  // row's draft and its head
+              dr -= i_first;
+              uint32_t bits = S.vis[bu][min(dr, i_last - i_first)][quad];
 #pragma unroll
-        for (int r = 0; r < RH; r += 2) {
-          const float4 q = *reinterpret_cast<const float4*>(&S.rcm[(r0 + r) / 2][0]);
-          fma2(v[r], v[r + 1], q.x, q.y, q.z, q.w);
-          tmax = fmaxf(tmax, fmaxf(v[r], v[r + 1]));
-        }
-        const bool unit = vm > 0.f && (vm > u * kUnitUp || vm < u * kUnitDown);  // the same in the group's threads
-        if (any_of(tmax > kLimit || unit, 3 + group, 128)) {
-          if (any_of(!ok, 3 + group, 128)) {  // a warp that gave up stays with the others' barriers until here: all of them leave
-            ok = false;
-            break;
-          }
-          // move the references to the maxima and the unit to the tile's largest V scale.  From the scores themselves:
-          // relative to the reference of a row that has seen nothing they have lost their digits
+              for (int r = 0; r < RC; ++r) {
+                if (!((bits >> lane) & 1u)) v[r] = -INFINITY;
+                if (++in == a.rep) {
+                  in = 0;
+                  ++dr;
+                  bits = S.vis[bu][min(dr, i_last - i_first)][quad];
+                }
+              }
+            }
+            if (!there) {
+#pragma unroll
+              for (int r = 0; r < RC; ++r) v[r] = -INFINITY;
+            }
+          };
           load_scores();
-          float x[RH];
+          float tmax = ok ? -INFINITY : INFINITY;
 #pragma unroll
-          for (int r = 0; r < RH; ++r) x[r] = v[r] = v[r] * S.rcm[(r0 + r) / 2][r & 1];
-          const float top = warp_reduce<RH, true>(x, lane);
-          S.wmax[quad][r0 + reduced_index<RH>(lane)] = top;
-          ptx::named_barrier(3 + group, 128);
-          const float u_new = unit ? vm : u;
-          if (const int r = r0 + quad * 32 + lane; r < r0 + RH) {
-            const float old = -S.rcm[r / 2][2 + (r & 1)];
-            const float m = fmaxf(fmaxf(old, fmaxf(S.wmax[0][r], S.wmax[1][r])), fmaxf(S.wmax[2][r], S.wmax[3][r]));
-            const float fl = exp2_fast(old - m);
-            S.rcm[r / 2][2 + (r & 1)] = -m;
-            S.fac_l[r] = fl;
-            S.fac_o[r] = fl * (u / u_new);
+          for (int r = 0; r < RC; r += 2) {
+            const float4 q = *reinterpret_cast<const float4*>(&S.rcm[(r0 + rc + r) / 2][0]);
+            fma2(v[r], v[r + 1], q.x, q.y, q.z, q.w);
+            tmax = fmaxf(tmax, fmaxf(v[r], v[r + 1]));
           }
-          ptx::named_barrier(3 + group, 128);
-          u = u_new;
+          float& u = unit_of[rc / RC];
+          const bool unit = vm > 0.f && (vm > u * kUnitUp || vm < u * kUnitDown);  // the same in the group's threads
+          if (any_of(tmax > kLimit || unit, 3 + group, 128)) {
+            if (any_of(!ok, 3 + group, 128)) {  // a warp that gave up stays with the others' barriers until here: all of them leave
+              leave = true;
+              break;
+            }
+            // move the references to the maxima and the unit to the tile's largest V scale.  From the scores themselves:
+            // relative to the reference of a row that has seen nothing they have lost their digits
+            load_scores();
+            float x[RC];
 #pragma unroll
-          for (int r = 0; r < RH; ++r) {
-            l[r] *= S.fac_l[r0 + r];
-            v[r] += S.rcm[(r0 + r) / 2][2 + (r & 1)];
-          }
-          if (it > 0) {
-            ok = wait_warp(&S.o_full, (it - 1) & 1, &S.abort, a.d.status, lane) && ok;  // the second product of tile it - 1 has ended
-            ptx::tc_fence_after();
-#pragma unroll 1
-            for (int c = 0; c < RH / 8; ++c) {
-              uint32_t o[8];
-              const uint32_t at = tmem + lane_base + C::kO + r0 + 8 * c;
-              tmem_ld8(at, o);
+            for (int r = 0; r < RC; ++r) x[r] = v[r] = v[r] * S.rcm[(r0 + rc + r) / 2][r & 1];
+            const float top = warp_reduce<RC, true>(x, lane);
+            S.wmax[quad][r0 + rc + reduced_index<RC>(lane)] = top;
+            ptx::named_barrier(3 + group, 128);
+            const float u_new = unit ? vm : u;
+            if (quad == 0 && lane < RC) {
+              const int r = r0 + rc + lane;
+              const float old = -S.rcm[r / 2][2 + (r & 1)];
+              const float m = fmaxf(fmaxf(old, fmaxf(S.wmax[0][r], S.wmax[1][r])), fmaxf(S.wmax[2][r], S.wmax[3][r]));
+              const float fl = exp2_fast(old - m);
+              S.rcm[r / 2][2 + (r & 1)] = -m;
+              S.fac_l[r] = fl;
+              S.fac_o[r] = fl * (u / u_new);
+            }
+            ptx::named_barrier(3 + group, 128);
+            u = u_new;
+#pragma unroll
+            for (int r = 0; r < RC; ++r) {
+              l[rc + r] *= S.fac_l[r0 + rc + r];
+              v[r] += S.rcm[(r0 + rc + r) / 2][2 + (r & 1)];
+            }
+            if (it > 0) {
+              ok = wait_warp(&S.o_full, (it - 1) & 1, &S.abort, a.d.status, lane) && ok;  // the second product of tile it - 1 has ended
+              ptx::tc_fence_after();
+              uint32_t o[RC];
+              const uint32_t at = tmem + lane_base + C::kO + r0 + rc;
+#pragma unroll
+              for (int c = 0; c < RC / 8; ++c) tmem_ld8(at + 8 * c, *reinterpret_cast<uint32_t(*)[8]>(o + 8 * c));
               ptx::tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * S.fac_o[r0 + 8 * c + e]);
-              tmem_st8(at, o);
+              for (int e = 0; e < RC; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * S.fac_o[r0 + rc + e]);
+#pragma unroll
+              for (int c = 0; c < RC / 8; ++c) tmem_st8(at + 8 * c, *reinterpret_cast<const uint32_t(*)[8]>(o + 8 * c));
+              tmem_st_wait();
             }
-            tmem_st_wait();
           }
-        }
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&S.s_empty[bu]);
-        const __half2 f = __float2half2_rn(u > 0.f ? v_scale / u : 0.f);
-        uint32_t p[RH / 2];
+          if (rc + RC == RH) {  // the scores have been read
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&S.s_empty[it % SB]);
+          }
+          const __half2 f = __float2half2_rn(u > 0.f ? v_scale / u : 0.f);
+          uint32_t p[RC / 2];
 #pragma unroll
-        for (int r = 0; r < RH; r += 2) {
-          const float p0 = exp2_fast(v[r]), p1 = exp2_fast(v[r + 1]);
-          add2(l[r], l[r + 1], p0, p1);
-          const __half2 h = __hmul2(__floats2half2_rn(p0, p1), f);
-          p[r / 2] = *reinterpret_cast<const uint32_t*>(&h);
-        }
-        // P and the widened V are free once the second product of the tile before has ended
-        if (it > 0) ok = wait_warp(&S.o_full, (it - 1) & 1, &S.abort, a.d.status, lane) && ok;
+          for (int r = 0; r < RC; r += 2) {
+            const float p0 = exp2_fast(v[r]), p1 = exp2_fast(v[r + 1]);
+            add2(l[rc + r], l[rc + r + 1], p0, p1);
+            const __half2 h = __hmul2(__floats2half2_rn(p0, p1), f);
+            p[r / 2] = *reinterpret_cast<const uint32_t*>(&h);
+          }
+          // a single P is free once the second product of the tile before has ended
+          if (C::kPBufs == 1 && it > 0 && rc == 0) ok = wait_warp(&S.o_full, (it - 1) & 1, &S.abort, a.d.status, lane) && ok;
 #pragma unroll
-        for (int c = 0; c < RH / 8; ++c)
-          *reinterpret_cast<uint4*>(p_row + (((r0 % 64) / 8 + c) ^ p_xor) * 16) = make_uint4(p[4 * c], p[4 * c + 1], p[4 * c + 2], p[4 * c + 3]);
+          for (int c = 0; c < RC / 8; ++c)
+            *reinterpret_cast<uint4*>(p_row + ((((r0 + rc) % 64) / 8 + c) ^ p_xor) * 16) = make_uint4(p[4 * c], p[4 * c + 1], p[4 * c + 2], p[4 * c + 3]);
+        }
+        if (leave) {
+          ok = false;
+          break;
+        }
+        if (C::kPBufs == 2 && it > 0) ok = wait_warp(&S.o_full, (it - 1) & 1, &S.abort, a.d.status, lane) && ok;  // the widened V is free
         // V: this thread's dimension (its lane of tensor memory), its group's share of the keys
         const int d = quad * 32 + lane;
         if (quad * 32 < D) {
@@ -639,7 +673,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
 #pragma unroll
           for (int z = 0; z < 8 / G; ++z) {
             const int seg = group * (8 / G) + z;
-            const uint4 w = *reinterpret_cast<const uint4*>(vt + v_piece<D>(d, seg, page_log2));
+            const uint4 w = *reinterpret_cast<const uint4*>(vt + v_off[z]);
             uint32_t ww[4] = {w.x, w.y, w.z, w.w};
             if (!plain) {
               // keys behind the end or without a page count as zero, so that 0 * V is 0; a NaN of a written key goes to the
@@ -685,6 +719,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         const bool split = a.chunks > 1;
 #pragma unroll 1
         for (int c = 0; c < RH / 8; ++c) {
+          const float u = RH > RC && c >= RC / 8 ? unit_of[RH / RC - 1] : unit_of[0];
           uint32_t oh[8];
           const uint32_t at = tmem + lane_base + C::kO + r0 + 8 * c;
           if (n_tiles > 0) {
