@@ -25,8 +25,12 @@
 //
 // Roles: one warp loads (TMA), one thread issues the MMAs, groups of four warps do the softmax of a share of the rows each
 // (tensor memory gives a warp a quarter of the lanes) and widen V.  S is double-buffered: S of tile i + 1 is computed
-// while the softmax works on tile i, the second product of tile i while it works on tile i + 1.  Work split: grid =
-// (chunks of the key range, kv head x row tiles, sequence); chunks meet in a second kernel (attend_combine), in order.
+// while the softmax works on tile i, the second product of tile i while it works on tile i + 1.  
+// Work split: all tiles of the call in one line (sequence, kv head, tile of rows, tile of keys), cut into equal
+// runs, one per CTA that the machine holds.  A run may end one (sequence, head, rows) segment, cover others and begin the
+// next: every CTA works equally long whatever the lengths, and sets up once or a few times.  A segment that lies in one run is
+// finished there; the others' parts meet in a second kernel (attend_combine), in order.  The lengths are device data,
+// so every CTA finds its run itself.  Segments of a few tiles (a window) are dealt out whole, without a second kernel.
 // Every wait is bounded.
 #pragma once
 #include <cuda.h>
@@ -54,10 +58,11 @@ struct Args {
   __nv_bfloat16* out;
   float* lse;          // [n_tokens, n_heads] or null
   const float* sinks;  // [n_heads] or null
-  float* part_o;       // [chunks, n_tokens, n_heads, D]
-  float2* part_ml;     // [chunks, n_tokens, n_heads]: maximum (base 2), denominator
+  int2* table;         // [n_seq + 1]: units and segments of the call before a sequence (written by the first CTA)
+  float2* part_ml;     // [slots][R]: maximum (base 2), denominator; slot = CTA + segment
+  float* part_o;       // [slots][R][D]
   long long q_stride, out_stride;
-  int n_heads, rep, row_tiles, chunks, chunk_keys, window;
+  int n_heads, rep, window, whole, grid;  // whole: a segment is one unit of work, not split
   float scale_log2;
 };
 
@@ -196,6 +201,20 @@ __device__ __forceinline__ uint32_t desc_lo(uint32_t addr) { return ((addr & 0x3
 __host__ __device__ constexpr uint32_t desc_hi(uint32_t stride, uint32_t layout) { return (stride >> 4) | (1u << 14) | (layout << 29); }
 constexpr uint32_t kSw128 = 2, kSw64 = 4, kSw32 = 6;
 
+// What a sequence brings: tiles of rows and tiles of keys; none without drafts.
+struct Extent {
+  int row_tiles, key_tiles;
+};
+__device__ __forceinline__ Extent extent(const Args& a, const Seq& s, int R) {
+  Extent e{0, 0};
+  if (s.n > 0) {
+    e.row_tiles = (s.n * a.rep + R - 1) / R;
+    e.key_tiles = (s.ctx + s.n - range_start(s, a.window) + kKeys - 1) / kKeys;
+  }
+  return e;
+}
+__device__ __forceinline__ int units_per_cta(int total, int grid) { return max(1, (int)(((unsigned)total + grid - 1) / (unsigned)grid)); }
+
 template <int D, int R>
 struct Cfg {
   static constexpr int kCtas = R <= 32 ? 2 : 1;  // per SM
@@ -233,6 +252,14 @@ struct Ctl {
   uint32_t nan_row[R][4];       // row's output is NaN in these dimensions
   int low[R], top[R];           // by draft of the tile: context keys > low are seen; a chain sees keys <= top
   int2 row[R];                  // token row, query head; -1: no row
+  int scan[2][20];              // sums of the warps' sequences: units, segments
+  int at_units, at_segs;        // before the sequence in which this CTA's run begins ...
+  int at_seq;                   // ... and that sequence
+  Seq at;
+  float fin[R];                 // what a row's accumulators are multiplied by in the end
+  float vmax[3];                // by V stage: largest V scale of the tile ...
+  int all_there[3];             // ... and whether each of its keys has a page
+  int any_nan;                  // some entry of nan_row is not zero
   uint32_t tmem;
   volatile int abort;
   volatile uint32_t k_it, v_it;  // tiles the loader armed (read on the abort path)
@@ -296,6 +323,66 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
     S.k_it = S.v_it = 0;
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int page_log2 = a.c.page_log2, page = 1 << page_log2;
+  const bool tree = a.d.parent != nullptr;
+  // ---- this CTA's run of units
+  int run, run_end, seq_units, seq_segs;  // position, end; units and segments before sequence b
+  int b;
+  Seq s;
+  {
+    constexpr int kWarps = C::kThreads / 32;
+    const int each = (a.d.n_seq + C::kThreads - 1) / C::kThreads, first = tid * each, last = min(a.d.n_seq, first + each);
+    auto weigh = [&](const Seq& q, int& units, int& segs) {
+      const Extent e = extent(a, q, R);
+      segs = e.row_tiles * a.c.heads;
+      units = a.whole ? segs : segs * e.key_tiles;
+    };
+    int un = 0, sg = 0;
+    Seq q{0, 0, 0};
+    for (int i = first; i < last; ++i) {
+      int u, g;
+      q = kv::sequence(a.d, i, page);
+      weigh(q, u, g);
+      un += u;
+      sg += g;
+    }
+    int iu = un, is = sg;  // inclusive sums over the threads
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int u1 = __shfl_up_sync(0xffffffffu, iu, o), s1 = __shfl_up_sync(0xffffffffu, is, o);
+      if (lane >= o) { iu += u1; is += s1; }
+    }
+    if (lane == 31) { S.scan[0][warp] = iu; S.scan[1][warp] = is; }
+    __syncthreads();
+    int total = 0, segs = 0, eu = iu - un, es = is - sg;  // eu, es: before this thread's sequences
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w == warp) { eu += total; es += segs; }
+      total += S.scan[0][w];
+      segs += S.scan[1][w];
+    }
+    const int per = units_per_cta(total, a.grid);
+    run = (int)min((long long)per * blockIdx.x, (long long)total);
+    run_end = min(run + per, total);
+    const bool tell = blockIdx.x == 0 && !a.whole, mine = run >= eu && run < eu + un;
+    if (tell || mine)
+      for (int i = first; i < last; ++i) {
+        int u, g;
+        if (each > 1) q = kv::sequence(a.d, i, page);
+        weigh(q, u, g);
+        if (tell) a.table[i] = make_int2(eu, es);
+        if (mine && run >= eu && run < eu + u) {
+          S.at_units = eu;
+          S.at_segs = es;
+          S.at_seq = i;
+          S.at = q;
+        }
+        eu += u;
+        es += g;
+      }
+    if (tell && tid == 0) a.table[a.d.n_seq] = make_int2(total, segs);
+    if (run >= run_end) return;  // the same for the whole CTA
+  }
   // Tensor memory is taken behind the wait and dependents are released behind that: no kernel holds tensor memory while
   // it waits for one that still has to take it.
   if (warp == 4 * G + 1) {
@@ -307,19 +394,25 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
   ptx::tc_fence_after();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tmem = S.tmem;
+  b = S.at_seq;
+  s = S.at;
+  seq_units = S.at_units;
+  seq_segs = S.at_segs;
 
-  const int page_log2 = a.c.page_log2, page = 1 << page_log2;
-  const int b = blockIdx.z, head = blockIdx.y / a.row_tiles, row0 = (blockIdx.y % a.row_tiles) * R;
-  const Seq s = kv::sequence(a.d, b, page);
-  const int n_rows = s.n * a.rep;
-  const int start = range_start(s, a.window);
-  const int k_begin = start + blockIdx.x * a.chunk_keys;
-  const int k_all = s.ctx + s.n;
-  const bool tree = a.d.parent != nullptr;
-  const bool work = row0 < n_rows && k_begin < k_all;
-  if (work) {
+  int gt = 0;  // tiles this CTA has been through: the barriers count on
+  for (int piece = 0; run < run_end; ++piece) {
+    Extent ext = extent(a, s, R);
+    const int in_seq = run - seq_units;
+    const int unit_tiles = a.whole ? 1 : ext.key_tiles;
+    const int seg_in_seq = in_seq / unit_tiles, first_tile = a.whole ? 0 : in_seq - seg_in_seq * unit_tiles;
+    const int head = seg_in_seq / ext.row_tiles, row0 = (seg_in_seq - head * ext.row_tiles) * R;
+    const int all_tiles = ext.key_tiles, piece_tiles = a.whole ? all_tiles : min(all_tiles - first_tile, run_end - run);
+    const bool split = piece_tiles < all_tiles;
+    const int slot = blockIdx.x + seq_segs + seg_in_seq;
+    const int n_rows = s.n * a.rep;
+    const int k_begin = range_start(s, a.window) + first_tile * kKeys, k_all = s.ctx + s.n;
     const int i_first = row0 / a.rep, i_last = min(n_rows - 1, row0 + R - 1) / a.rep;
-    int k_end = min(k_begin + a.chunk_keys, k_all);
+    int k_end = min(k_begin + piece_tiles * kKeys, k_all);
     if (!tree) k_end = min(k_end, s.ctx + i_last + 1);  // a chain: nobody here sees later drafts
     const int n_tiles = k_end > k_begin ? (k_end - k_begin + kKeys - 1) / kKeys : 0;
     const int low_max = a.window > 0 ? s.ctx + s.n - 1 - a.window : -1;
@@ -339,39 +432,47 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
       };
       // page ids two tiles ahead, scales one: each is a trip to memory that the copies do not wait for
       auto scale_at = [&](int p, float& k, float& v) {
-        const long long slot = (long long)max(p, 0) * a.c.heads + head;
-        k = p >= 0 ? __ldg(a.c.ks + slot) : 0.f;
-        v = p >= 0 ? __ldg(a.c.vs + slot) : 0.f;
+        const long long at = (long long)max(p, 0) * a.c.heads + head;
+        k = p >= 0 ? a.c.ks[at] : 0.f;
+        v = p >= 0 ? a.c.vs[at] : 0.f;
       };
       int pid = page_at(0), pid1 = page_at(1);
       float ks, vs;
       scale_at(pid, ks, vs);
       for (int it = 0; it < n_tiles; ++it) {
-        const int sk = it % KS, sv = it % VS;
+        const int ct = gt + it, sk = ct % KS, sv = ct % VS;
         const int pid2 = page_at(it + 2);
         float ks1, vs1;
         scale_at(pid1, ks1, vs1);
         const int mine = __shfl_sync(0xffffffffu, pid, ((lane & 7) << page_log2) >> 4 & 7);  // page `lane` of the tile
         const bool on = lane < pages && mine >= 0;
         const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, on)) * page * D;
-        if (it >= KS && !wait_warp(&S.k_empty[sk], ((it / KS) & 1) ^ 1, &S.abort, a.d.status, lane)) break;
+        if (ct >= KS && !wait_warp(&S.k_empty[sk], ((ct / KS) & 1) ^ 1, &S.abort, a.d.status, lane)) break;
         uint8_t* dst = smem + C::oK + sk * C::kTile + (lane & 7) * page * D;
         if (lane == 0) {
           ptx::mbar_arrive_expect_tx(&S.k_full[sk], bytes);
-          S.k_it = it + 1;
+          S.k_it = ct + 1;
         }
         __syncwarp();
         if (on) ptx::tma_load_2d(dst, &tm_k, &S.k_full[sk], 0, (mine * a.c.heads + head) << page_log2, ptx::kPolicyEvictNormal);
-        if (it >= VS && !wait_warp(&S.v_empty[sv], ((it / VS) & 1) ^ 1, &S.abort, a.d.status, lane)) break;
+        if (ct >= VS && !wait_warp(&S.v_empty[sv], ((ct / VS) & 1) ^ 1, &S.abort, a.d.status, lane)) break;
         if (lane < 8) {
           S.ks[sv][lane] = ks;
           S.vs[sv][lane] = vs;
           S.pid[sv][lane] = pid;
         }
+        float top = vs;  // lanes 0..7 hold the tile's pieces, and the others copies
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const bool there = __all_sync(0xffffffffu, pid >= 0);
+        if (lane == 0) {
+          S.vmax[sv] = top;
+          S.all_there[sv] = there;
+        }
         __syncwarp();
         if (lane == 0) {
           ptx::mbar_arrive_expect_tx(&S.v_full[sv], bytes);
-          S.v_it = it + 1;
+          S.v_it = ct + 1;
         }
         __syncwarp();
         dst = smem + C::oV + sv * C::kTile + (lane & 7) * page * D;
@@ -394,9 +495,9 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         constexpr uint32_t kHi = desc_hi(8 * D, D == 128 ? kSw128 : kSw64), pHi = desc_hi(8 * C::kPRow, C::kPRow == 128 ? kSw128 : C::kPRow == 64 ? kSw64 : kSw32);
         bool ok = true;
         auto scores = [&](int it) {
-          const int st = it % KS, u = it % SB;
-          ok = ok && wait(&S.k_full[st], (it / KS) & 1, &S.abort, a.d.status);
-          if (it >= SB) ok = ok && wait(&S.s_empty[u], ((it / SB) & 1) ^ 1, &S.abort, a.d.status);
+          const int ct = gt + it, st = ct % KS, u = ct % SB;
+          ok = ok && wait(&S.k_full[st], (ct / KS) & 1, &S.abort, a.d.status);
+          if (ct >= SB) ok = ok && wait(&S.s_empty[u], ((ct / SB) & 1) ^ 1, &S.abort, a.d.status);
           if (!ok) return;
           ptx::tc_fence_after();
           const uint32_t ka = kb + st * (C::kTile / 16);
@@ -408,18 +509,18 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
           ptx::mma_commit(&S.k_empty[st]);
           ptx::mma_commit(&S.s_full[u]);
         };
-        if (n_tiles > 0) {
-          ok = wait(&S.q_full, 0, &S.abort, a.d.status);
-          scores(0);
+        {
+          ok = wait(&S.q_full, piece & 1, &S.abort, a.d.status);
+          if (n_tiles > 0) scores(0);
         }
         for (int it = 0; it < n_tiles && ok; ++it) {
           if (it + 1 < n_tiles) scores(it + 1);
-          ok = ok && wait(&S.p_full, it & 1, &S.abort, a.d.status);
+          ok = ok && wait(&S.p_full, (gt + it) & 1, &S.abort, a.d.status);
           if (!ok) break;
           ptx::tc_fence_after();
 #pragma unroll
           for (int k = 0; k < kKeys / 16; ++k)
-            mma_f16_ta(tmem + C::kO, tmem + C::kV16 + k * 8, pb + (it % C::kPBufs) * (C::kP / 16) + k * C::kPRow, pHi, pdesc, it + k > 0);  // 16 keys on
+            mma_f16_ta(tmem + C::kO, tmem + C::kV16 + k * 8, pb + ((gt + it) % C::kPBufs) * (C::kP / 16) + k * C::kPRow, pHi, pdesc, it + k > 0);  // 16 keys on
           ptx::mma_commit(&S.o_full);
         }
         if (!ok) {  // abort: what was issued must have ended before tensor memory and shared memory are given back
@@ -449,14 +550,30 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         S.top[tid] = tree ? s.ctx - 1 : at;
       }
       for (int i = tid; i < R * 4; i += NS) (&S.nan_row[0][0])[i] = 0;
-      // Q: a row's D elements by D / 8 neighbouring lanes, 8 each
-      constexpr int kPer = D / 8;
-      for (int z = tid; z < R * kPer; z += NS) {
-        const int r = z / kPer, d0 = (z % kPer) * 8, rr = row0 + r;
+      if (tid == 0) S.any_nan = 0;
+      // Q: a row's D elements by D / 8 neighbouring lanes, 8 each; all loads first
+      constexpr int kPer = D / 8, kItems = R * kPer / NS > 0 ? R * kPer / NS : 1;
+      uint4 raw[kItems];
+#pragma unroll
+      for (int k = 0; k < kItems; ++k) {
+        const int z = k * NS + tid, rr = row0 + z / kPer;
+        raw[k] = make_uint4(0, 0, 0, 0);
+        if (z < R * kPer && rr < n_rows)
+          raw[k] = *reinterpret_cast<const uint4*>(a.q + (long long)(s.lo + rr / a.rep) * a.q_stride + (long long)(head * a.rep + rr % a.rep) * D + (z % kPer) * 8);
+      }
+#pragma unroll
+      for (int k = 0; k < kItems; ++k) {
+        const int z = k * NS + tid, r = z / kPer, d0 = (z % kPer) * 8, rr = row0 + r;
+        if (R * kPer < NS && z >= R * kPer) break;
         const bool live = rr < n_rows;
         const int i = rr / a.rep, hq = head * a.rep + rr % a.rep;
-        float v[8] = {};
-        if (live) kv::load8(a.q + (long long)(s.lo + i) * a.q_stride + (long long)hq * D + d0, v);
+        const uint32_t u4[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[2 * e] = __uint_as_float(u4[e] << 16);
+          v[2 * e + 1] = __uint_as_float(u4[e] & 0xffff0000u);
+        }
         float m = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e]));
@@ -467,26 +584,33 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         const int ex = (int)(__float_as_uint(m) >> 23) - 127;
         float up = 1.f, back = 1.f;
         if (ex >= -110 && ex < 128) {
-          up = ldexpf(1.f, 7 - ex);
-          back = ldexpf(1.f, ex - 7);
+          up = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
+          back = __uint_as_float((uint32_t)(127 + ex - 7) << 23);
         }
         if ((z % kPer) == 0) {
           S.rcm[r / 2][r & 1] = a.scale_log2 * back;
           S.rcm[r / 2][2 + (r & 1)] = -kUnseen;
           S.row[r] = live ? make_int2(s.lo + i, hq) : make_int2(-1, 0);
         }
-        uint32_t code[3][2] = {};
+        if (ex == 128) {  // infinities become NaN: a row with one has NaN scores, as inf * 0 and inf - inf have it
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float x = v[e] * up;
+          for (int e = 0; e < 8; ++e) v[e] = fabsf(v[e]) == INFINITY ? __int_as_float(0x7fffffff) : v[e];
+        }
+        uint32_t code[3][2];
 #pragma unroll
-          for (int term = 0; term < 3; ++term) {
-            // infinities become NaN: a row with one has NaN scores, as inf * 0 and inf - inf have it
-            const __nv_fp8_storage_t c = fabsf(x) <= 448.f ? __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3) : (__nv_fp8_storage_t)0x7F;
-            const __half_raw h = __nv_cvt_fp8_to_halfraw(c, __NV_E4M3);
-            x -= __half2float(*reinterpret_cast<const __half*>(&h));
-            code[term][e >> 2] |= (uint32_t)c << (8 * (e & 3));
+        for (int e = 0; e < 8; e += 2) mul2(v[e], v[e + 1], up);
+#pragma unroll
+        for (int term = 0; term < 3; ++term) {
+          uint32_t c[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            c[e] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v[2 * e], v[2 * e + 1]), __NV_SATFINITE, __NV_E4M3);
+            const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)c[e], __NV_E4M3);
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+            add2(v[2 * e], v[2 * e + 1], -f.x, -f.y);
           }
+          code[term][0] = c[0] | c[1] << 16;
+          code[term][1] = c[2] | c[3] << 16;
         }
 #pragma unroll
         for (int term = 0; term < 3; ++term)
@@ -499,9 +623,9 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
       float l[RH];
 #pragma unroll
       for (int r = 0; r < RH; ++r) l[r] = 0.f;
-      float unit_of[RH / RC];  // V scale that the accumulators of each part of the rows are in units of
+      float unit_of[RH / RC], inv_of[RH / RC];  // V scale that the accumulators of each part of the rows are in units of, its reciprocal
 #pragma unroll
-      for (int c = 0; c < RH / RC; ++c) unit_of[c] = 0.f;
+      for (int c = 0; c < RH / RC; ++c) unit_of[c] = inv_of[c] = 0.f;
       const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
       // this key's row of P; 16-byte piece c of it is at c ^ p_xor
       uint8_t* const p_row0 = smem + C::oP + (r0 / 64) * C::kPBlock + key * C::kPRow;
@@ -511,7 +635,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
       for (int z = 0; z < 8 / G; ++z) v_off[z] = v_piece<D>(quad * 32 + lane, group * (8 / G) + z, page_log2);
       bool ok = true;
       for (int it = 0; it < n_tiles; ++it) {
-        const int sv = it % VS, bu = it & 1;
+        const int ct = gt + it, sv = ct % VS, bu = ct & 1;
         const int k0 = k_begin + it * kKeys;
         const bool masked = k0 + kKeys > s.ctx || k0 <= low_max;  // somebody may not see a key of the tile
         if (masked) {
@@ -531,37 +655,33 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
           }
           ptx::named_barrier(3 + group, 128);
         }
-        ok = wait_warp(&S.v_full[sv], (it / VS) & 1, &S.abort, a.d.status, lane) && ok;
-        ok = wait_warp(&S.s_full[it % SB], (it / SB) & 1, &S.abort, a.d.status, lane) && ok;
+        ok = wait_warp(&S.v_full[sv], (ct / VS) & 1, &S.abort, a.d.status, lane) && ok;
+        ok = wait_warp(&S.s_full[ct % SB], (ct / SB) & 1, &S.abort, a.d.status, lane) && ok;
         ptx::tc_fence_after();
         const float k_scale = S.ks[sv][key >> 4], v_scale = S.vs[sv][key >> 4];
         const bool there = S.pid[sv][key >> 4] >= 0;
-        float vm;
-        bool plain = !masked;  // every key is there and every row sees it
-        {
-          const float4 x = *reinterpret_cast<const float4*>(&S.vs[sv][0]), y = *reinterpret_cast<const float4*>(&S.vs[sv][4]);
-          vm = fmaxf(fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)), fmaxf(fmaxf(y.x, y.y), fmaxf(y.z, y.w)));
-          const int4 i = *reinterpret_cast<const int4*>(&S.pid[sv][0]), j = *reinterpret_cast<const int4*>(&S.pid[sv][4]);
-          plain = plain && (i.x | i.y | i.z | i.w | j.x | j.y | j.z | j.w) >= 0;
-        }
-        const uint32_t s_at = tmem + lane_base + (it % SB) * C::kSCols + r0;
-        uint8_t* const p_row = p_row0 + (it % C::kPBufs) * C::kP;
+        const float vm = S.vmax[sv];
+        const bool plain = !masked && S.all_there[sv];  // every key is there and every row sees it
+        const uint32_t s_at = tmem + lane_base + (ct % SB) * C::kSCols + r0;
+        uint8_t* const p_row = p_row0 + (ct % C::kPBufs) * C::kP;
         bool leave = false;
 #pragma unroll
         for (int rc = 0; rc < RH; rc += RC) {  // RC of this thread's rows at a time
           float v[RC];
           auto load_scores = [&]() {  // times the page's scale; -inf where the row does not see this thread's key
-            float w[RC];
+            constexpr int kTerms = C::kSCols / R;
+            float w[kTerms][RC];
 #pragma unroll
-            for (int term = 0; term < C::kSCols / R; ++term) {
-              float* const to = term ? w : v;
+            for (int term = 0; term < kTerms; ++term)
 #pragma unroll
-              for (int c = 0; c < RC / 8; ++c) tmem_ld8(s_at + term * R + rc + 8 * c, *reinterpret_cast<uint32_t(*)[8]>(to + 8 * c));
-              ptx::tmem_ld_wait();
-              if (term) {
+              for (int c = 0; c < RC / 8; ++c) tmem_ld8(s_at + term * R + rc + 8 * c, *reinterpret_cast<uint32_t(*)[8]>(&w[term][8 * c]));
+            ptx::tmem_ld_wait();
 #pragma unroll
-                for (int r = 0; r < RC; r += 2) add2(v[r], v[r + 1], w[r], w[r + 1]);
-              }
+            for (int r = 0; r < RC; r += 2) {
+              v[r] = w[0][r];
+              v[r + 1] = w[0][r + 1];
+#pragma unroll
+              for (int term = 1; term < kTerms; ++term) add2(v[r], v[r + 1], w[term][r], w[term][r + 1]);
             }
 #pragma unroll
             for (int r = 0; r < RC; r += 2) mul2(v[r], v[r + 1], k_scale);
@@ -620,13 +740,14 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
             }
             ptx::named_barrier(3 + group, 128);
             u = u_new;
+            inv_of[rc / RC] = u > 0.f ? 1.f / u : 0.f;
 #pragma unroll
             for (int r = 0; r < RC; ++r) {
               l[rc + r] *= S.fac_l[r0 + rc + r];
               v[r] += S.rcm[(r0 + rc + r) / 2][2 + (r & 1)];
             }
             if (it > 0) {
-              ok = wait_warp(&S.o_full, (it - 1) & 1, &S.abort, a.d.status, lane) && ok;  // the second product of tile it - 1 has ended
+              ok = wait_warp(&S.o_full, (ct - 1) & 1, &S.abort, a.d.status, lane) && ok;  // the second product of tile it - 1 has ended
               ptx::tc_fence_after();
               uint32_t o[RC];
               const uint32_t at = tmem + lane_base + C::kO + r0 + rc;
@@ -643,9 +764,9 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
           if (rc + RC == RH) {  // the scores have been read
             ptx::tc_fence_before();
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&S.s_empty[it % SB]);
+            if (lane == 0) ptx::mbar_arrive(&S.s_empty[ct % SB]);
           }
-          const __half2 f = __float2half2_rn(u > 0.f ? v_scale / u : 0.f);
+          const __half2 f = __float2half2_rn(v_scale * inv_of[rc / RC]);
           uint32_t p[RC / 2];
 #pragma unroll
           for (int r = 0; r < RC; r += 2) {
@@ -655,7 +776,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
             p[r / 2] = *reinterpret_cast<const uint32_t*>(&h);
           }
           // a single P is free once the second product of the tile before has ended
-          if (C::kPBufs == 1 && it > 0 && rc == 0) ok = wait_warp(&S.o_full, (it - 1) & 1, &S.abort, a.d.status, lane) && ok;
+          if (C::kPBufs == 1 && it > 0 && rc == 0) ok = wait_warp(&S.o_full, (ct - 1) & 1, &S.abort, a.d.status, lane) && ok;
 #pragma unroll
           for (int c = 0; c < RC / 8; ++c)
             *reinterpret_cast<uint4*>(p_row + ((((r0 + rc) % 64) / 8 + c) ^ p_xor) * 16) = make_uint4(p[4 * c], p[4 * c + 1], p[4 * c + 2], p[4 * c + 3]);
@@ -664,7 +785,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
           ok = false;
           break;
         }
-        if (C::kPBufs == 2 && it > 0) ok = wait_warp(&S.o_full, (it - 1) & 1, &S.abort, a.d.status, lane) && ok;  // the widened V is free
+        if (C::kPBufs == 2 && it > 0) ok = wait_warp(&S.o_full, (ct - 1) & 1, &S.abort, a.d.status, lane) && ok;  // the widened V is free
         // V: this thread's dimension (its lane of tensor memory), its group's share of the keys
         const int d = quad * 32 + lane;
         if (quad * 32 < D) {
@@ -690,7 +811,10 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
                     if ((bad >> (8 * y)) & 1u) {
                       const int kk = seg * 16 + 4 * e + y;
                       for (int r = 0; r < R && row0 + r < n_rows; ++r)
-                        if ((S.vis[bu][(row0 + r) / a.rep - i_first][kk >> 5] >> (kk & 31)) & 1u) atomicOr(&S.nan_row[r][d >> 5], 1u << (d & 31));
+                        if ((S.vis[bu][(row0 + r) / a.rep - i_first][kk >> 5] >> (kk & 31)) & 1u) {
+                          atomicOr(&S.nan_row[r][d >> 5], 1u << (d & 31));
+                          S.any_nan = 1;
+                        }
                     }
                 }
               }
@@ -710,57 +834,86 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         }
       }
       // ---- results
-      if (ok && n_tiles > 0) ok = wait_warp(&S.o_full, (n_tiles - 1) & 1, &S.abort, a.d.status, lane);
+      if (ok && n_tiles > 0) ok = wait_warp(&S.o_full, (gt + n_tiles - 1) & 1, &S.abort, a.d.status, lane);
       ptx::tc_fence_after();
       const float sum = warp_reduce<RH, false>(l, lane);
       S.lsum[quad][r0 + reduced_index<RH>(lane)] = sum;
       if (!any_of(!ok, 3 + group, 128)) {
-        const int d = quad * 32 + lane;
-        const bool split = a.chunks > 1;
-#pragma unroll 1
-        for (int c = 0; c < RH / 8; ++c) {
-          const float u = RH > RC && c >= RC / 8 ? unit_of[RH / RC - 1] : unit_of[0];
-          uint32_t oh[8];
-          const uint32_t at = tmem + lane_base + C::kO + r0 + 8 * c;
-          if (n_tiles > 0) {
-            tmem_ld8(at, oh);
-            ptx::tmem_ld_wait();
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) oh[e] = 0u;
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int r = r0 + 8 * c + e;
-            const int2 ro = S.row[r];
-            if (ro.x < 0 || d >= D) continue;
-            float den = (S.lsum[0][r] + S.lsum[1][r]) + (S.lsum[2][r] + S.lsum[3][r]);
-            float m = den == 0.f ? -INFINITY : -S.rcm[r / 2][2 + (r & 1)];
-            float o = __uint_as_float(oh[e]) * u;
-            if ((S.nan_row[r][d >> 5] >> (d & 31)) & 1u) o = __int_as_float(0x7fffffff);
-            if (split) {
-              const long long w = ((long long)blockIdx.x * a.d.n_tokens + ro.x) * a.n_heads + ro.y;
-              a.part_o[w * D + d] = o;
-              if (d == 0) a.part_ml[w] = make_float2(m, den);
-            } else {
+        // one thread per row: its denominator, and what its accumulators are multiplied by
+        if (const int r = r0 + quad * 32 + lane; r < r0 + RH) {
+          const int2 ro = S.row[r];
+          float den = (S.lsum[0][r] + S.lsum[1][r]) + (S.lsum[2][r] + S.lsum[3][r]);
+          float m = den == 0.f ? -INFINITY : -S.rcm[r / 2][2 + (r & 1)];
+          float fin = RH > RC && r - r0 >= RC ? unit_of[RH / RC - 1] : unit_of[0];
+          if (ro.x >= 0) {
+            if (split) a.part_ml[(long long)slot * R + r] = make_float2(m, den);
+            else {
               if (a.sinks) {
                 const float sk = a.sinks[ro.y] * 1.4426950408889634f, mm = fmaxf(m, sk), g = exp2_fast(m - mm);
                 den = den * g + exp2_fast(sk - mm);
-                o *= g;
+                fin *= g;
                 m = mm;
               }
-              const float inv = den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den);
-              a.out[(long long)ro.x * a.out_stride + (long long)ro.y * D + d] = __float2bfloat16_rn(o * inv);
-              if (d == 0 && a.lse) a.lse[(long long)ro.x * a.n_heads + ro.y] = den == 0.f ? -INFINITY : (m + log2f(den)) * 0.6931471805599453f;
+              fin *= den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den);
+              if (a.lse) a.lse[(long long)ro.x * a.n_heads + ro.y] = den == 0.f ? -INFINITY : (m + log2f(den)) * 0.6931471805599453f;
+            }
+          }
+          S.fin[r] = fin;
+        }
+        ptx::named_barrier(3 + group, 128);
+        const int d = quad * 32 + lane;
+        if (quad * 32 < D) {
+          const bool nans = S.any_nan != 0;
+          float* part = a.part_o + ((long long)slot * R + r0) * D + d;
+#pragma unroll
+          for (int c = 0; c < RH; c += 8) {
+            uint32_t oh[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+            if (n_tiles > 0) {
+              tmem_ld8(tmem + lane_base + C::kO + r0 + c, oh);
+              ptx::tmem_ld_wait();
+            }
+            float o[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = __uint_as_float(oh[e]) * S.fin[r0 + c + e];
+            if (nans) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if ((S.nan_row[r0 + c + e][d >> 5] >> (d & 31)) & 1u) o[e] = __int_as_float(0x7fffffff);
+            }
+            if (split) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) part[(c + e) * D] = o[e];  // rows that are not there have room, too
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const int2 ro = S.row[r0 + c + e];
+                if (ro.x >= 0) a.out[(long long)ro.x * a.out_stride + (long long)ro.y * D + d] = __float2bfloat16_rn(o[e]);
+              }
             }
           }
         }
       }
     }
-    if (S.abort && warp == 4 * G && lane == 0) {  // copies in flight land before the shared memory is given back
-      ptx::drain_ring(S.k_full, KS, S.k_it, kBudgetNs);
-      ptx::drain_ring(S.v_full, VS, S.v_it, kBudgetNs);
+    // ---- on to the next piece: everybody has left this one
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    if (S.abort) break;
+    gt += n_tiles;
+    run += a.whole ? 1 : piece_tiles;
+    const int seq_all = ext.row_tiles * a.c.heads * (a.whole ? 1 : ext.key_tiles);
+    if (run < run_end && run >= seq_units + seq_all) {  // the run goes on in another sequence
+      seq_units += seq_all;
+      do {
+        seq_segs += ext.row_tiles * a.c.heads;
+        s = kv::sequence(a.d, ++b, page);
+        ext = extent(a, s, R);
+      } while (ext.row_tiles == 0);  // units are left: a sequence with drafts follows
     }
+  }
+  if (S.abort && warp == 4 * G && lane == 0) {  // copies in flight land before the shared memory is given back
+    ptx::drain_ring(S.k_full, KS, S.k_it, kBudgetNs);
+    ptx::drain_ring(S.v_full, VS, S.v_it, kBudgetNs);
   }
   ptx::tc_fence_before();
   __syncthreads();
@@ -768,9 +921,9 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
   if (warp == 4 * G + 1) ptx::tmem_dealloc(tmem, C::kTmem);
 }
 
-// One warp per (token, head): the chunks' parts, in order, and the sink.
+// One warp per (token, head): the parts of its segment, in order, and the sink.  A segment of one part was finished there.
 template <int D>
-__global__ void __launch_bounds__(128) attend_combine_kernel(const Args a) {
+__global__ void __launch_bounds__(128) attend_combine_kernel(const Args a, const int R) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int lane = threadIdx.x & 31, b = blockIdx.z, hq = blockIdx.y * 4 + (threadIdx.x >> 5);
@@ -778,38 +931,61 @@ __global__ void __launch_bounds__(128) attend_combine_kernel(const Args a) {
   const Seq s = kv::sequence(a.d, b, 1 << a.c.page_log2);
   const int i = blockIdx.x;
   if (i >= s.n) return;
-  const int span = s.ctx + s.n - range_start(s, a.window);
-  const int chunks = (span + a.chunk_keys - 1) / a.chunk_keys;
-  const long long token = s.lo + i, step = (long long)a.d.n_tokens * a.n_heads;
-  const long long at = token * a.n_heads + hq;
+  const Extent ext = extent(a, s, R);
+  const int head = hq / a.rep, rr = i * a.rep + hq - head * a.rep;
+  const int2 before = a.table[b];
+  const int per = units_per_cta(a.table[a.d.n_seq].x, a.grid);
+  const int seg = head * ext.row_tiles + rr / R, from = before.x + seg * ext.key_tiles;
+  const int c0 = from / per, parts = (from + ext.key_tiles - 1) / per - c0 + 1;
+  if (parts == 1) return;
+  const long long token = s.lo + i, at = (long long)(c0 + before.y + seg) * R + rr % R;  // row of the first part; R further on that of the next
   float m = -INFINITY;
-  for (int c = lane; c < chunks; c += 32) m = fmaxf(m, a.part_ml[at + c * step].x);
+  for (int c = lane; c < parts; c += 32) m = fmaxf(m, a.part_ml[at + (long long)c * R].x);
 #pragma unroll
   for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
   if (a.sinks) m = fmaxf(m, a.sinks[hq] * 1.4426950408889634f);
   const float mr = m == -INFINITY ? 0.f : m;
-  constexpr int V = D / 32;
+  constexpr int V = D / 32, kBatch = 8;  // parts in flight
   float o[V] = {}, den = 0.f;
-  for (int c = 0; c < chunks; ++c) {
-    const float2 ml = a.part_ml[at + c * step];
-    if (ml.y == 0.f) continue;  // nothing seen in this chunk
-    const float w = exp2_fast(ml.x - mr);
-    den = fmaf(w, ml.y, den);
-    const float* p = a.part_o + (at + c * step) * D + lane * V;
-    if constexpr (V == 4) {
-      const float4 v = *reinterpret_cast<const float4*>(p);
-      o[0] = fmaf(w, v.x, o[0]); o[1] = fmaf(w, v.y, o[1]); o[2] = fmaf(w, v.z, o[2]); o[3] = fmaf(w, v.w, o[3]);
-    } else {
-      const float2 v = *reinterpret_cast<const float2*>(p);
-      o[0] = fmaf(w, v.x, o[0]); o[1] = fmaf(w, v.y, o[1]);
+  const long long step = (long long)R * D;
+  const float* p = a.part_o + at * D + lane * V;
+  for (int c0p = 0; c0p < parts; c0p += 32) {  // a lane has a part's weight, all lanes its columns
+    const int c = c0p + lane;
+    float w = 0.f;
+    if (c < parts) {
+      const float2 ml = a.part_ml[at + (long long)c * R];
+      w = exp2_fast(ml.x - mr);
+      den = fmaf(w, ml.y, den);
+    }
+    const int n = min(32, parts - c0p);
+    for (int k = 0; k < n; k += kBatch) {
+      float v[kBatch][V];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[j][e] = 0.f;
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+        if (k + j < n) {
+          if constexpr (V == 4) *reinterpret_cast<float4*>(v[j]) = *reinterpret_cast<const float4*>(p + (c0p + k + j) * step);
+          else *reinterpret_cast<float2*>(v[j]) = *reinterpret_cast<const float2*>(p + (c0p + k + j) * step);
+        }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const float wj = __shfl_sync(0xffffffffu, w, (k + j) & 31);
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = fmaf(wj, v[j][e], o[e]);
+      }
     }
   }
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) den += __shfl_xor_sync(0xffffffffu, den, x);
   if (a.sinks) den += exp2_fast(a.sinks[hq] * 1.4426950408889634f - mr);
   const float inv = den > 0.f ? 1.f / den : (den == 0.f ? 0.f : den);
   __nv_bfloat16* out = a.out + token * a.out_stride + (long long)hq * D + lane * V;
 #pragma unroll
   for (int e = 0; e < V; e += 2) *reinterpret_cast<__nv_bfloat162*>(out + e) = __floats2bfloat162_rn(o[e] * inv, o[e + 1] * inv);
-  if (a.lse && lane == 0) a.lse[at] = den == 0.f ? -INFINITY : (m + log2f(den)) * 0.6931471805599453f;
+  if (a.lse && lane == 0) a.lse[token * a.n_heads + hq] = den == 0.f ? -INFINITY : (m + log2f(den)) * 0.6931471805599453f;
 }
 
 }  // namespace att

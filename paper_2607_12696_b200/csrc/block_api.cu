@@ -28,7 +28,9 @@ int sm_count() {
 template <typename... KArgs, typename... Args>
 cudaError_t launch(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
   if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    // without this the driver may leave an SM shared memory for one CTA where two fit
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (e != cudaSuccess) return e;
   }
   cudaLaunchConfig_t cfg = {};
@@ -153,7 +155,9 @@ kv::Cache cache_of(const moev_kv_cache* c) {
 }
 
 struct Plan {
-  int rows, row_tiles, chunks, chunk_keys;  // rows of a tile
+  int rows, grid, whole;  // rows of a tile, CTAs, segments dealt out whole
+  long long units;        // tiles of the call, at most
+  size_t table, ml, o;    // bytes of the workspace's parts
 };
 Plan attend_plan(const moev_kv_cache* c, const moev_draft_batch* d, int n_heads, int window) {
   Plan p;
@@ -162,23 +166,17 @@ Plan attend_plan(const moev_kv_cache* c, const moev_draft_batch* d, int n_heads,
   p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   // a tile of 128 rows and the ancestors of very large trees do not fit together
   if (p.rows == 128 && att::smem_bytes<128, 128>((d->max_drafts + 31) / 32, d->parent != nullptr) > 227 * 1024) p.rows = 64;
-  p.row_tiles = (int)((rows + p.rows - 1) / p.rows);
   long long span = d->max_len;
   if (window > 0) span = std::min<long long>(span, (long long)window + d->max_drafts + att::kKeys - 1);
-  const long long base = (long long)std::max(1, d->n_seq) * c->n_kv_heads * p.row_tiles;
-  const int slots = sm_count() * (p.rows <= 32 ? 2 : 1);
-  // one wave of CTAs while that splits the keys at all; with many sequences or heads several waves, whose
-  // chunks even out their different lengths, but no chunk below 1024 keys
-  long long want, least = att::kKeys;
-  if (base * 2 <= slots) want = slots / base;
-  else {
-    want = (4LL * slots + base - 1) / base;
-    least = 1024;
-  }
-  long long keys = std::max<long long>((span + want - 1) / want, least);
-  keys = (keys + att::kKeys - 1) / att::kKeys * att::kKeys;
-  p.chunk_keys = (int)keys;
-  p.chunks = (int)((span + keys - 1) / keys);
+  const long long tiles = (span + att::kKeys - 1) / att::kKeys;  // of keys, at most
+  const long long segments = (long long)d->n_seq * c->n_kv_heads * ((rows + p.rows - 1) / p.rows);
+  p.whole = tiles <= 4;
+  p.units = segments * tiles;
+  p.grid = (int)std::min<long long>(sm_count() * (p.rows <= 32 ? 2 : 1), p.whole ? segments : segments * tiles);
+  const size_t slots = (size_t)p.grid + (size_t)segments;
+  p.table = p.whole ? 0 : (((size_t)d->n_seq + 1) * 8 + 15) & ~(size_t)15;
+  p.ml = p.whole ? 0 : slots * p.rows * 8;
+  p.o = p.whole ? 0 : slots * p.rows * c->head_dim * 4;
   return p;
 }
 
@@ -210,7 +208,7 @@ bool encode_rows(CUtensorMap* m, const void* ptr, int width, long long rows, int
 template <int D, int R>
 cudaError_t launch_attend(const att::Args& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t st) {
   const size_t smem = att::smem_bytes<D, R>((a.d.max_drafts + 31) / 32, a.d.parent != nullptr);
-  return launch(att::attend_kernel<D, R>, dim3(a.chunks, a.c.heads * a.row_tiles, a.d.n_seq), dim3(att::Cfg<D, R>::kThreads), smem, st, a, tk, tv);
+  return launch(att::attend_kernel<D, R>, dim3(a.grid), dim3(att::Cfg<D, R>::kThreads), smem, st, a, tk, tv);
 }
 template <int D>
 cudaError_t launch_attend_d(const att::Args& a, int rows, cudaStream_t st) {
@@ -223,8 +221,8 @@ cudaError_t launch_attend_d(const att::Args& a, int rows, cudaStream_t st) {
   else if (rows == 32) e = launch_attend<D, 32>(a, tk, tv, st);
   else if (rows == 64) e = launch_attend<D, 64>(a, tk, tv, st);
   else e = launch_attend<D, 128>(a, tk, tv, st);
-  if (e != cudaSuccess || a.chunks == 1) return e;
-  return launch(att::attend_combine_kernel<D>, dim3(a.d.max_drafts, (a.n_heads + 3) / 4, a.d.n_seq), dim3(128), 0, st, a);
+  if (e != cudaSuccess || a.whole) return e;
+  return launch(att::attend_combine_kernel<D>, dim3(a.d.max_drafts, (a.n_heads + 3) / 4, a.d.n_seq), dim3(128), 0, st, a, rows);
 }
 
 }  // namespace
@@ -349,7 +347,7 @@ moev_status moev_cache_append(const moev_kv_cache* c, const moev_draft_batch* d,
 size_t moev_cache_attend_workspace(const moev_kv_cache* c, const moev_draft_batch* d, int32_t n_heads, int32_t window) {
   if (!batch_ok(c, d) || n_heads < 1 || n_heads % c->n_kv_heads) return 0;
   const Plan p = attend_plan(c, d, n_heads, window);
-  return p.chunks > 1 ? (size_t)p.chunks * d->n_tokens * n_heads * (c->head_dim + 2) * 4 : 0;
+  return p.table + p.ml + p.o;
 }
 
 moev_status moev_cache_attend(const moev_kv_cache* c, const moev_draft_batch* d, const void* q, int64_t q_stride, int32_t n_heads, float scale,
@@ -361,9 +359,9 @@ moev_status moev_cache_attend(const moev_kv_cache* c, const moev_draft_batch* d,
   if (d->n_tokens > 1 && (q_stride < row || out_stride < row)) return MOEV_EINVAL;
   if (d->n_seq == 0 || d->n_tokens == 0) return MOEV_OK;
   const Plan p = attend_plan(c, d, n_heads, window);
-  if ((long long)c->n_kv_heads * p.row_tiles > 65535 || (n_heads + 3) / 4 > 65535) return MOEV_EINVAL;
-  const size_t parts = (size_t)p.chunks * d->n_tokens * n_heads;
-  if (p.chunks > 1 && (!workspace || !aligned(workspace, 16) || workspace_bytes < parts * (c->head_dim + 2) * 4)) return MOEV_EINVAL;
+  if ((n_heads + 3) / 4 > 65535 || p.units > 0x3fffffffLL) return MOEV_EINVAL;
+  const size_t need = p.table + p.ml + p.o;
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return MOEV_EINVAL;
   att::Args a{};
   a.d = drafts_of(d);
   a.c = cache_of(c);
@@ -371,16 +369,17 @@ moev_status moev_cache_attend(const moev_kv_cache* c, const moev_draft_batch* d,
   a.out = static_cast<__nv_bfloat16*>(out);
   a.lse = lse;
   a.sinks = sinks;
-  a.part_o = static_cast<float*>(workspace);
-  a.part_ml = reinterpret_cast<float2*>(static_cast<float*>(workspace) + parts * c->head_dim);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  a.table = reinterpret_cast<int2*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(ws + p.table);
+  a.part_o = reinterpret_cast<float*>(ws + p.table + p.ml);
   a.q_stride = q_stride;
   a.out_stride = out_stride;
   a.n_heads = n_heads;
   a.rep = n_heads / c->n_kv_heads;
-  a.row_tiles = p.row_tiles;
-  a.chunks = p.chunks;
-  a.chunk_keys = p.chunk_keys;
   a.window = window;
+  a.whole = p.whole;
+  a.grid = p.grid;
   a.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   return done(c->head_dim == 64 ? launch_attend_d<64>(a, p.rows, st) : launch_attend_d<128>(a, p.rows, st));

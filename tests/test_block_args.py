@@ -98,7 +98,8 @@ def test_cache_calls_refuse_arguments():
 def test_attend_refuses_a_small_workspace():
     c, b = C.byref(cache(n_pages=4000)), C.byref(batch(max_len=40000, table_cols=2500))
     size = L.moev_cache_attend_workspace(c, b, 4, 0)
-    assert size > 0 and size % (3 * 4 * 66 * 4) == 0  # chunks x tokens x heads x (D + 2) floats
+    # sequences + 1 entries of 8 bytes, and a tile of 16 rows of D + 2 floats per CTA and per (sequence, head, rows) segment
+    assert size > 0 and (size - 16) % (16 * 66 * 4) == 0
     for ws, n in ((None, size), (BASE + 8, size), (BASE, size - 1)):
         assert L.moev_cache_attend(c, b, BASE, 256, 4, 0.1, 0, None, BASE, 256, None, ws, n, None) == 1
 
