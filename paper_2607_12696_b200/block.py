@@ -1,8 +1,9 @@
 """The operators around the MoE layer (second part of include/moev.h) on torch tensors.
 
 Like the rest of the package these functions check and marshal arguments; every step runs in the
-library's kernels, asynchronously on torch's current stream.  A call whose tensors do not fit raises
-:class:`MoevError` (``MOEV_EINVAL``) before anything is launched.
+library's kernels, asynchronously on torch's current stream.  The checks are compiled
+(``csrc/block_py.cpp``): a small call's kernels take less time than the same checks in Python.  A call
+whose tensors do not fit raises :class:`MoevError` (``MOEV_EINVAL``) before anything is launched.
 """
 from __future__ import annotations
 
@@ -10,74 +11,38 @@ import ctypes as C
 
 import torch
 
-from .binding import (ACT_BF16, ACT_FP32, ACTQ_NONE, W_INT4, W_MXFP4, MoevError, _DraftBatch, _KvCache, _Linear, _Norm, lib)
+from .binding import ACTQ_NONE, W_INT4, W_MXFP4, MoevError, _DraftBatch, _KvCache, _Linear, lib
 
-_AFMT = {torch.bfloat16: ACT_BF16, torch.float32: ACT_FP32}
 _EINVAL = 1
-_raw_stream = torch._C._cuda_getCurrentRawStream
+_ext = None
+
+
+def _fast():
+    """The compiled checks (``_block``); like the library itself they have no fallback."""
+    global _ext
+    if _ext is None:
+        lib()
+        from . import _block
+        _ext = _block
+    return _ext
 
 
 def _bad(text: str):
     raise MoevError(_EINVAL, text)
 
 
-def _stream(t: torch.Tensor) -> int:
-    """Raw handle of the current stream; the kernels run on the current device."""
-    dev = t.get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
-        _bad(f"tensors must be on the current CUDA device, got {t.device}")
-    return _raw_stream(dev)
-
-
 def _same_device(first: torch.Tensor, *others):
-    dev = first.get_device()
     for t in others:
-        if t is not None and t.get_device() != dev:
+        if t is not None and t.device != first.device:
             _bad(f"tensors on different devices: {first.device} and {t.device}")
-
-
-def _rows(t: torch.Tensor, name: str, n: int, width: int, dtype) -> int:
-    """Row stride of a tensor whose first dimension is rows and whose others are contiguous (``width`` elements)."""
-    if t.dtype != dtype or t.dim() < 2 or t.shape[0] != n or t.numel() != n * width:
-        _bad(f"{name}: expected {n} rows of {width} {dtype}, got {tuple(t.shape)} {t.dtype}")
-    step = 1
-    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if size != 1 and stride != step:
-            _bad(f"{name}: everything behind the first dimension must be contiguous, got strides {t.stride()}")
-        step *= size
-    return t.stride(0) if n > 1 else width
 
 
 def add_rmsnorm(x: torch.Tensor, weight: torch.Tensor, out: dict, residual: torch.Tensor = None, eps: float = 1e-6,
                 act_quant: int = ACTQ_NONE) -> dict:
     """moev_add_rmsnorm: ``out`` maps "y" / "residual" / "codes" / "scales" to the tensors that are wanted
     (codes uint8 or float8_e4m3fn [n, H] and scales float32 [n, ceil(H / 128)] exactly with ``act_quant``)."""
-    if x.dim() != 2 or x.dtype not in _AFMT:
-        _bad(f"x: expected a bfloat16 or float32 matrix, got {tuple(x.shape)} {x.dtype}")
-    n, H = x.shape
-    y, ro, codes, scales = out.get("y"), out.get("residual"), out.get("codes"), out.get("scales")
-    _same_device(x, weight, residual, y, ro, codes, scales)
-    if weight.dtype not in _AFMT or weight.shape != (H,) or not weight.is_contiguous():
-        _bad(f"weight: expected {H} contiguous bfloat16 or float32 values")
-    p = _Norm(n=n, H=H, afmt=_AFMT[x.dtype], wfmt=_AFMT[weight.dtype], eps=eps, act_quant=act_quant, x=x.data_ptr(), w=weight.data_ptr(),
-              x_stride=_rows(x, "x", n, H, x.dtype))
-    if residual is not None:
-        p.residual, p.residual_stride = residual.data_ptr(), _rows(residual, "residual", n, H, x.dtype)
-    if y is not None:
-        p.y, p.y_stride = y.data_ptr(), _rows(y, "y", n, H, x.dtype)
-    if ro is not None:
-        p.residual_out, p.residual_out_stride = ro.data_ptr(), _rows(ro, "out residual", n, H, x.dtype)
-    if codes is not None:
-        if codes.dtype not in (torch.uint8, torch.float8_e4m3fn):
-            _bad(f"codes: expected uint8 or float8_e4m3fn, got {codes.dtype}")
-        p.codes, p.codes_stride = codes.data_ptr(), _rows(codes, "codes", n, H, codes.dtype)
-    if scales is not None:
-        if scales.dtype != torch.float32 or scales.shape != (n, (H + 127) // 128) or not scales.is_contiguous():
-            _bad(f"scales: expected contiguous float32 [{n}, {(H + 127) // 128}]")
-        p.scales = scales.data_ptr()
-    st = lib().moev_add_rmsnorm(C.byref(p), _stream(x))
-    if st != 0:
-        raise MoevError(st, "moev_add_rmsnorm rejected the call")
+    get = out.get
+    (_ext or _fast()).add_rmsnorm(x, weight, residual, get("y"), get("residual"), get("codes"), get("scales"), eps, act_quant)
     return out
 
 
@@ -100,31 +65,20 @@ class W4Linear:
         if bias is not None and (bias.dtype != torch.float32 or bias.shape != (N,) or not bias.is_contiguous()):
             _bad(f"bias: expected contiguous float32 [{N}]")
         _same_device(codes, scales, bias)
+        dev = codes.get_device()
+        if dev < 0 or dev != torch.cuda.current_device():
+            _bad(f"tensors must be on the current CUDA device, got {codes.device}")
         self.bias = bias
-        stream = _stream(codes)
         self.packed = torch.empty(size, dtype=torch.uint8, device=codes.device)
-        st = lib().moev_w4_pack(C.byref(self._c), codes.data_ptr(), scales.data_ptr(), self.packed.data_ptr(), stream)
+        st = lib().moev_w4_pack(C.byref(self._c), codes.data_ptr(), scales.data_ptr(), self.packed.data_ptr(),
+                                C.c_void_p(torch.cuda.current_stream().cuda_stream))
         if st != 0:
             raise MoevError(st, "moev_w4_pack rejected the weight")
-        self._ref = C.byref(self._c)
-        self._packed_ptr = self.packed.data_ptr()
-        self._bias_ptr = None if bias is None else bias.data_ptr()
-        self._dev = codes.get_device()
+        self._args = (C.addressof(self._c), self.packed.data_ptr(), 0 if bias is None else bias.data_ptr(), dev)
 
     def __call__(self, x: torch.Tensor, y: torch.Tensor = None) -> torch.Tensor:
         """moev_linear_w4: x bfloat16 [n, K] -> y bfloat16 or float32 [n, N] (allocated as bfloat16 when not given)."""
-        n = x.shape[0]
-        if y is None:
-            y = torch.empty(n, self.N, dtype=torch.bfloat16, device=x.device)
-        if y.dtype not in _AFMT:
-            _bad(f"y: expected bfloat16 or float32, got {y.dtype}")
-        if x.get_device() != self._dev or y.get_device() != self._dev:
-            _bad(f"x and y must be on the weight's device cuda:{self._dev}")
-        st = lib().moev_linear_w4(self._ref, self._packed_ptr, self._bias_ptr, x.data_ptr(), _rows(x, "x", n, self.K, torch.bfloat16), n,
-                                  y.data_ptr(), _rows(y, "y", n, self.N, y.dtype), _AFMT[y.dtype], _stream(x))
-        if st != 0:
-            raise MoevError(st, "moev_linear_w4 rejected the call")
-        return y
+        return (_ext or _fast()).linear_w4(*self._args, x, y)
 
 
 class KvCache:
@@ -147,7 +101,8 @@ class KvCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.n_kv_heads, self.page, self.head_dim = n, heads, page, D
         self._c = _KvCache(n, page, heads, D, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
-        self._ref = C.byref(self._c)
+        self._at = C.addressof(self._c)
+        self._dev = k.get_device()
 
     @classmethod
     def empty(cls, n_pages: int, page: int, n_kv_heads: int, head_dim: int, device="cuda") -> "KvCache":
@@ -174,68 +129,40 @@ class DraftBatch:
         self.max_drafts, self.max_len = max_drafts, max_len
         self._c = _DraftBatch(n, 0, max_drafts, max_len, page_table.shape[1], cu.data_ptr(), ctx_len.data_ptr(), page_table.data_ptr(),
                               None if parent is None else parent.data_ptr(), None if status is None else status.data_ptr())
-        self._ref = C.byref(self._c)
+        self._at = C.addressof(self._c)
+        self._parents = 0 if parent is None else parent.numel()
+        self._dev = cu.get_device()
 
-    def _for(self, n_tokens: int):
-        if self.parent is not None and self.parent.numel() < n_tokens:
-            _bad(f"parent has {self.parent.numel()} entries for {n_tokens} token rows")
-        self._c.n_tokens = n_tokens
-        return self._ref
+
+def _together(cache: KvCache, batch: DraftBatch):
+    if cache._dev != batch._dev:
+        _bad(f"cache and batch on different devices: {cache.k.device} and {batch.cu.device}")
 
 
 def cache_append(cache: KvCache, batch: DraftBatch, k: torch.Tensor, v: torch.Tensor, rope: torch.Tensor = None, q: torch.Tensor = None,
                  q_out: torch.Tensor = None):
     """moev_cache_append: k, v bfloat16 [n_tokens, heads, D]; rope float32 [positions, D] (cosines, sines); q bfloat16
     [n_tokens, query heads, D], rotated into q_out (default: in place).  Returns q_out."""
-    T, D, heads = k.shape[0], cache.head_dim, cache.n_kv_heads
-    bf16 = torch.bfloat16
-    n_heads, q_ptr, q_stride, o_ptr, o_stride = 0, None, 0, None, 0
-    if q is not None:
-        q_out = q if q_out is None else q_out
-        n_heads = q.numel() // (T * D) if T else heads
-        q_ptr, q_stride = q.data_ptr(), _rows(q, "q", T, n_heads * D, bf16)
-        o_ptr, o_stride = q_out.data_ptr(), _rows(q_out, "q_out", T, n_heads * D, bf16)
-    if rope is not None and (rope.dtype != torch.float32 or rope.dim() != 2 or rope.shape[1] != D or not rope.is_contiguous()):
-        _bad(f"rope: expected contiguous float32 [positions, {D}]")
-    _same_device(k, v, cache.k, batch.cu, rope, q, q_out)
-    st = lib().moev_cache_append(cache._ref, batch._for(T), k.data_ptr(), _rows(k, "k", T, heads * D, bf16), v.data_ptr(),
-                                 _rows(v, "v", T, heads * D, bf16), None if rope is None else rope.data_ptr(),
-                                 0 if rope is None else rope.shape[0], q_ptr, q_stride, n_heads, o_ptr, o_stride, _stream(k))
-    if st != 0:
-        raise MoevError(st, "moev_cache_append rejected the call (alignment, strides, head counts or bounds)")
-    return q_out
+    if cache._dev != batch._dev:
+        _together(cache, batch)
+    return (_ext or _fast()).cache_append(cache._at, batch._at, batch._parents, cache._dev, k, v, rope, q, q_out)
 
 
-def cache_attend_workspace(cache: KvCache, batch: DraftBatch, n_heads: int, window: int = 0, n_tokens: int = None) -> torch.Tensor:
-    """A workspace for cache_attend calls of this size (``n_tokens`` rows; by default one full tree per sequence)."""
-    n = batch.ctx_len.numel() * batch.max_drafts if n_tokens is None else n_tokens
-    batch._c.n_tokens = n
-    size = lib().moev_cache_attend_workspace(cache._ref, batch._ref, n_heads, window)
+def cache_attend_workspace(cache: KvCache, batch: DraftBatch, n_heads: int, window: int = 0) -> torch.Tensor:
+    """A workspace for cache_attend calls with these bounds (it does not depend on the number of token rows)."""
+    size = lib().moev_cache_attend_workspace(C.byref(cache._c), C.byref(batch._c), n_heads, window)
     return torch.empty(size, dtype=torch.uint8, device=cache.k.device)
 
 
 def cache_attend(cache: KvCache, batch: DraftBatch, q: torch.Tensor, out: torch.Tensor = None, lse: torch.Tensor = None, scale: float = None,
                  window: int = 0, sinks: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
     """moev_cache_attend: q, out bfloat16 [n_tokens, query heads, D]; lse float32 [n_tokens, query heads]; sinks float32
-    [query heads].  Without a workspace that is large enough, one is taken from torch's allocator for the call."""
-    T, D = q.shape[0], cache.head_dim
-    n_heads = q.numel() // (T * D) if T else cache.n_kv_heads
-    if out is None:
-        out = torch.zeros_like(q)
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (T, n_heads) or not lse.is_contiguous()):
-        _bad(f"lse: expected contiguous float32 [{T}, {n_heads}]")
-    if sinks is not None and (sinks.dtype != torch.float32 or sinks.shape != (n_heads,) or not sinks.is_contiguous()):
-        _bad(f"sinks: expected contiguous float32 [{n_heads}]")
-    _same_device(q, cache.k, batch.cu, out, lse, sinks, workspace)
-    b = batch._for(T)
-    q_stride, o_stride = _rows(q, "q", T, n_heads * D, torch.bfloat16), _rows(out, "out", T, n_heads * D, torch.bfloat16)
-    L = lib()
-    size = L.moev_cache_attend_workspace(cache._ref, b, n_heads, window)
-    if size and (workspace is None or workspace.numel() * workspace.element_size() < size):
-        workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
-    st = L.moev_cache_attend(cache._ref, b, q.data_ptr(), q_stride, n_heads, D ** -0.5 if scale is None else scale, window,
-                             None if sinks is None else sinks.data_ptr(), out.data_ptr(), o_stride, None if lse is None else lse.data_ptr(),
-                             workspace.data_ptr() if size else None, size, _stream(q))
-    if st != 0:
-        raise MoevError(st, "moev_cache_attend rejected the call (alignment, strides, head counts, scale or bounds)")
-    return out
+    [query heads]; scale defaults to D ** -0.5.  Without a workspace that is large enough, one is taken from torch's
+    allocator for the call."""
+    if cache._dev != batch._dev:
+        _together(cache, batch)
+    if scale is None:
+        scale = 0.0
+    elif scale == 0.0:
+        _bad("scale: expected a positive number")
+    return (_ext or _fast()).cache_attend(cache._at, batch._at, batch._parents, cache._dev, q, out, lse, scale, window, sinks, workspace)

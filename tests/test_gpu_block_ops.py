@@ -373,7 +373,7 @@ def test_captured_and_replayed():
     step(c2, d2, None)
     for t, u in ((c.k, c2.k), (c.v, c2.v), (c.k_scale, c2.k_scale), (c.v_scale, c2.v_scale)):
         t.copy_(u)
-    ws = moev.cache_attend_workspace(c, d, 8, n_tokens=s.T)
+    ws = moev.cache_attend_workspace(c, d, 8)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
