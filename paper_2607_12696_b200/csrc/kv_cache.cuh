@@ -65,7 +65,7 @@ struct AppendArgs {
   __nv_bfloat16* q_out;
   long long k_stride, v_stride, q_stride, q_out_stride;
   const float* rope;  // [rope_rows, D]: D / 2 cosines, then D / 2 sines
-  int rope_rows, rep;  // rep: query heads per kv head, 0 = no q
+  int rope_rows, rep, q_parts;  // rep: query heads per kv head, 0 = no q; q_parts: CTAs that share a page's queries
 };
 
 __device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8]) {
@@ -132,7 +132,8 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
 // One CTA per (page that a sequence's drafts touch, kv head, sequence).  The page's new rows are read
 // twice, once for the largest magnitude and once to be written, the second time from the caches; the
 // codes pass through shared memory, where those of V are turned from token rows into dimension rows.
-// The CTA also rotates the query heads of its kv head for the tokens of its page.
+// Further CTAs of the page and head rotate the query heads of the group for the page's tokens, two thirds of the bytes
+// at 8 query heads a kv head.
 // Bound by memory: 2 (Hq + 2 Hkv) D bytes in, 2 Hq D + 2 Hkv D out per token.
 template <int D>
 __global__ void __launch_bounds__(256) cache_append_kernel(const AppendArgs a) {
@@ -141,7 +142,9 @@ __global__ void __launch_bounds__(256) cache_append_kernel(const AppendArgs a) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int page = 1 << a.c.page_log2;
-  const int b = blockIdx.z, head = blockIdx.y, tid = threadIdx.x;
+  // roles: K and V of a page and head (part 0), or a share of the queries of its group (parts 1 ..)
+  // The part is the slowest index: the longer K and V CTAs start first.
+  const int b = blockIdx.y, part = blockIdx.z / a.c.heads, head = blockIdx.z - part * a.c.heads, tid = threadIdx.x;
   const Seq s = sequence(a.d, b, page);
   const int col = (s.ctx >> a.c.page_log2) + blockIdx.x;
   const int first = max(s.ctx, col << a.c.page_log2), last = min(s.ctx + s.n, (col + 1) << a.c.page_log2);
@@ -173,6 +176,33 @@ __global__ void __launch_bounds__(256) cache_append_kernel(const AppendArgs a) {
     __syncthreads();
   }
   constexpr int kHalf = D / 16;  // pieces of 8 columns in half a row; a thread takes one and its partner
+  if (part > 0) {
+    const int items = m * a.rep * kHalf, step = a.q_parts * blockDim.x;
+    constexpr int kBatch = 2;  // items whose loads are in flight
+    for (int z0 = (part - 1) * blockDim.x + tid; z0 < items; z0 += kBatch * step) {
+      float x[kBatch][8], y[kBatch][8];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int z = z0 + k * step;
+        if (z < items) {
+          const int rr = z / kHalf, r = rr / a.rep;
+          load_rotated<D>(a.q + (s.lo + i0 + r) * a.q_stride + (head * a.rep + rr - r * a.rep) * D, a.rope ? a.rope + (long long)pos[r] * D : nullptr,
+                          (z % kHalf) * 8, x[k], y[k]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int z = z0 + k * step;
+        if (z < items) {
+          const int rr = z / kHalf, r = rr / a.rep;
+          __nv_bfloat16* o = a.q_out + (s.lo + i0 + r) * a.q_out_stride + (head * a.rep + rr - r * a.rep) * D + (z % kHalf) * 8;
+          store8(o, x[k]);
+          store8(o + D / 2, y[k]);
+        }
+      }
+    }
+    return;
+  }
   const __nv_bfloat16* krow = a.k + (long long)(s.lo + i0) * a.k_stride + head * D;
   const __nv_bfloat16* vrow = a.v + (long long)(s.lo + i0) * a.v_stride + head * D;
   float mk = 0.f, mv = 0.f;
@@ -219,12 +249,25 @@ __global__ void __launch_bounds__(256) cache_append_kernel(const AppendArgs a) {
       }
       *reinterpret_cast<uint2*>(kc + r * D + c) = make_uint2(u[0], u[1]);
       *reinterpret_cast<uint2*>(kc + r * D + c + D / 2) = make_uint2(u[2], u[3]);
-      load_rotated<D>(vrow + (long long)r * a.v_stride, nullptr, c, x, y);
+    }
+    // V: a thread takes four neighbouring slots and 8 dimensions, and writes words of four tokens.  Of 32 lanes 8 are
+    // neighbours in the slots and 4 in the dimensions: 64-byte runs of global memory, 32 banks of shared memory.
+    const int g0 = fill >> 2, groups = ((fill + m + 3) >> 2) - g0;
+    for (int z = tid; z < ((groups + 7) & ~7) * (D / 8); z += blockDim.x) {
+      const int block = z >> 5, g = (block / (D / 32)) * 8 + (z & 7), c = ((block % (D / 32)) * 4 + ((z >> 3) & 3)) * 8;
+      if (g >= groups) continue;
+      uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        vc[(c + i) * v_pitch + fill + r] = (uint8_t)cache_code(x[i], v_inv);
-        vc[(c + i + D / 2) * v_pitch + fill + r] = (uint8_t)cache_code(y[i], v_inv);
+      for (int k = 0; k < 4; ++k) {
+        const int r = 4 * (g0 + g) + k - fill;
+        if (r < 0 || r >= m) continue;
+        float x[8];
+        load8(vrow + (long long)r * a.v_stride + c, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] |= cache_code(x[i], v_inv) << (8 * k);
       }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) *reinterpret_cast<uint32_t*>(vc + (c + i) * v_pitch + 4 * (g0 + g)) = w[i];
     }
     __syncthreads();
     // K: the new rows are one contiguous run; the kept rows only where the scale grew
@@ -257,17 +300,6 @@ __global__ void __launch_bounds__(256) cache_append_kernel(const AppendArgs a) {
         *p = (kept & low) | (was & high) | (fresh & ~(low | high));
       }
     }
-  }
-  // queries of this kv head's group
-  const int rows = m * a.rep;
-  for (int z = tid; z < rows * kHalf; z += blockDim.x) {
-    const int rr = z / kHalf, c = (z % kHalf) * 8, r = rr / a.rep, h = head * a.rep + rr % a.rep;
-    const long long token = s.lo + i0 + r;
-    float x[8], y[8];
-    load_rotated<D>(a.q + token * a.q_stride + h * D, a.rope ? a.rope + (long long)pos[r] * D : nullptr, c, x, y);
-    __nv_bfloat16* o = a.q_out + token * a.q_out_stride + h * D + c;
-    store8(o, x);
-    store8(o + D / 2, y);
   }
 }
 

@@ -129,6 +129,17 @@ __global__ void __launch_bounds__(512) add_rmsnorm_kernel(NormArgs a) {
       if (c < H) norm_store8<T, VEC>(ro, c, H, v[p]);
     }
   }
+  // w is on its way while the row's sum is taken
+  const TW* w = static_cast<const TW*>(a.w);
+  constexpr bool kEarly = VEC && sizeof(TW) == 2 && PV <= 2;
+  uint4 wq[kEarly ? PV : 1];
+  if constexpr (kEarly) {
+#pragma unroll
+    for (int p = 0; p < PV; ++p) {
+      const int c = (p * blockDim.x + tid) * 8;
+      if (c < H) wq[p] = *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(w) + c);
+    }
+  }
 #pragma unroll
   for (int p = 0; p < PV; ++p)
 #pragma unroll
@@ -140,7 +151,6 @@ __global__ void __launch_bounds__(512) add_rmsnorm_kernel(NormArgs a) {
   for (int i = 0; i < (int)(blockDim.x >> 5); ++i) tot += part[i];  // same order in every thread
   const float rs = 1.f / sqrtf(tot / (float)H + a.eps);
 
-  const TW* w = static_cast<const TW*>(a.w);
   T* y = a.y ? static_cast<T*>(a.y) + row * a.y_stride : nullptr;
 #pragma unroll
   for (int p = 0; p < PV; ++p) {
@@ -148,7 +158,16 @@ __global__ void __launch_bounds__(512) add_rmsnorm_kernel(NormArgs a) {
     const bool in = c < H;
     if (in) {
       float g[8];
-      norm_load8<TW, VEC>(w, c, H, g);
+      if constexpr (kEarly) {
+        const uint32_t u[4] = {wq[p].x, wq[p].y, wq[p].z, wq[p].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          g[2 * i] = __uint_as_float(u[i] << 16);
+          g[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+        }
+      } else {
+        norm_load8<TW, VEC>(w, c, H, g);
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[p][i] = v[p][i] * rs * g[i];
       if (y) norm_store8<T, VEC>(y, c, H, v[p]);
@@ -162,21 +181,21 @@ __global__ void __launch_bounds__(512) add_rmsnorm_kernel(NormArgs a) {
       for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(lanes, m, o));
       const float s = act_scale(m, a.quant);
       if (in) {
-        uint32_t q[2] = {0u, 0u};
-        if (a.quant == 2) {  // a power of two: the product with its reciprocal is the quotient, exactly
-          const float inv = 1.f / s;
-          if (s >= 1.17549435e-38f && inv >= 1.17549435e-38f) {
+        float t[8];
+        if (a.quant == 2 && s >= 1.17549435e-38f && s <= 8.5070592e37f) {
+          // a power of two with a normal reciprocal: the product with that is the quotient, exactly
+          const float inv = __uint_as_float(0x7F000000u - __float_as_uint(s));
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              q[i >> 2] |= (uint32_t)__nv_cvt_float_to_fp8(v[p][i] * inv, __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) q[i >> 2] |= act_code(v[p][i], s) << (8 * (i & 3));
-          }
+          for (int i = 0; i < 8; ++i) t[i] = v[p][i] * inv;
         } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) q[i >> 2] |= act_code(v[p][i], s) << (8 * (i & 3));
+          for (int i = 0; i < 8; ++i) t[i] = __fdiv_rn(v[p][i], s);
         }
+        uint32_t q[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          q[i] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(t[4 * i], t[4 * i + 1]), __NV_SATFINITE, __NV_E4M3) |
+                 (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(t[4 * i + 2], t[4 * i + 3]), __NV_SATFINITE, __NV_E4M3) << 16;
         uint8_t* cr = a.codes + row * a.codes_stride;
         if constexpr (VEC) *reinterpret_cast<uint2*>(cr + c) = make_uint2(q[0], q[1]);
         else
