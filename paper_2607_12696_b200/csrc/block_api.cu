@@ -94,8 +94,8 @@ cudaError_t launch_linear(const w4::Args& a0, cudaStream_t st) {
   const int warps = 16;
   int kw = 1;
   while (kw < 16 && 2 * kw <= a.n_chunks && tiles * kw * 10 < sms * warps * 6) kw *= 2;
-  // bytes of a piece of x: a row is 256 bytes a chunk + 64 (rows then start in alternating halves of the banks), a scale 2
-  auto piece_bytes = [&](int chunks) { return (size_t)rows * (chunks * 256 + 64) + (size_t)chunks * 16 * NT; };
+  // bytes of a piece of x: a row is 256 bytes a chunk + 64 (rows then start in alternating halves of the banks), MXFP4 has scales behind them
+  auto piece_bytes = [&](int chunks) { return (size_t)rows * (chunks * 256 + 64) + (FMT == w4::kMx ? (size_t)chunks * 16 * NT : 0); };
   const size_t most = 227 * 1024, red = (size_t)warps * NT * 8 * w4::kRedPitch * 4;
   int grid, piece;
   for (;; kw /= 2) {
@@ -116,7 +116,8 @@ cudaError_t launch_linear(const w4::Args& a0, cudaStream_t st) {
     a.red_at = apart ? a.n_bufs * a.buf_bytes : 0;
     break;
   }
-  a.kw = kw;
+  a.kw_log2 = 0;
+  while ((1 << a.kw_log2) < kw) ++a.kw_log2;
   a.phase_chunks = a.n_bufs == 1 ? (a.n_chunks + kw - 1) / kw * kw : piece;
   a.x_pitch = piece * 256 + 64;
   const size_t smem = std::max((size_t)a.n_bufs * a.buf_bytes, a.red_at + (kw > 1 ? red : 0));

@@ -3,12 +3,12 @@
 //   INT4:  W[o, k] = (q[o, k] - 8) * s[o, k / group]     q in 0..15, s bf16, group 32, 64 or 128
 //   MXFP4: W[o, k] = e2m1(q[o, k]) * 2^(s[o, k / 32] - 127)
 //
-// mma.sync m16n8k16 with f16 operands and binary32 accumulators.  The codes are exact in f16.  x (bf16) is
-// brought to f16 by a power of two per row and chunk of 128 k, its largest element to [2^14, 2^15), so that an element
-// keeps all its 8 significant bits down to 2^-28 of the largest (and is off by at most 2^-40 of that below): the
-// products are exact.  They are added over one group, multiplied by the binary32 scale, added over the chunk, and
-// that is multiplied by the chunk's power of two and added to the output: no weight and no sum is rounded to fewer
-// bits.  f16 and not bf16 because its 10 mantissa bits take two code positions of a word each without a shift.
+// mma.sync m16n8k16 with binary32 accumulators; products are exact, they are added over one group, multiplied by the
+// binary32 scale and added to the output: no weight and no sum is rounded to fewer bits.
+//   INT4 in bf16: the codes are exact, x is taken as it is.
+//   MXFP4 in f16, where sign and magnitude of an e2m1 code are in place after one shift.  x is brought to f16 by a power of
+//   two per row and chunk of 128 k, its largest element to [2^14, 2^15), so that an element keeps all its 8 significant bits
+//   down to 2^-28 of the largest (and is off by at most 2^-40 of that below).
 // Bound by the weight stream (N K / 2 bytes + scales) and, close behind, by the instructions that unpack it.
 //
 // Packed layout (made once per weight, moev_w4_pack).  The weights are the A operand (16 outputs x
@@ -40,7 +40,7 @@ struct Args {
   long long x_stride, y_stride;
   int n, N, K, n_chunks;   // n: rows of x in all
   int rounds;              // tiles per warp, one after another
-  int kw;                  // warps that share a tile's K
+  int kw_log2;             // warps that share a tile's K
   int phase_chunks;        // chunks of K per staged piece of x (a multiple of kw)
   int x_pitch;             // bytes per staged row
   int buf_bytes;           // bytes per staged piece of x
@@ -57,21 +57,16 @@ __device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t bits) {
   return r;
 }
 
-// 8 codes of a word -> 4 f16 pairs, pair p = k 2 p and 2 p + 1.  MXFP4: 2^-14 times the value.
+// 8 codes of a word -> 4 pairs, pair p = k 2 p and 2 p + 1.  INT4: bf16.  MXFP4: f16, 2^-14 times the value.
 template <int FMT>
 __device__ __forceinline__ void decode(uint32_t w, uint32_t magic, uint32_t (&r)[4]) {
   if constexpr (FMT == kInt4) {
-    // nibble p = k 2 p, nibble p + 4 = k 2 p + 1.  0x6400 | q is 1024 + q and 0x6400 | q << 4 is 1024 + 16 q: one
-    // exact subtraction or fused multiply-add from q - 8.
-    const uint32_t v = w >> 8;
-    const uint32_t u[4] = {and_or<0x000F000Fu>(w, magic), and_or<0x00F000F0u>(w, magic), and_or<0x000F000Fu>(v, magic), and_or<0x00F000F0u>(v, magic)};
-    const __half2 off = __half2half2(__ushort_as_half(0x6408)), sixteenth = __half2half2(__ushort_as_half(0x2C00)),
-                  off16 = __half2half2(__ushort_as_half(0xD480));  // 1032, 1 / 16, -72
+    // nibble p = k 2 p, nibble p + 4 = k 2 p + 1.  0x4300 | q is 128 + q; minus 136 is exact.
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-      __half2 h = *reinterpret_cast<const __half2*>(&u[p]);
-      h = p & 1 ? __hfma2(h, sixteenth, off16) : __hsub2(h, off);
-      r[p] = *reinterpret_cast<uint32_t*>(&h);
+      const uint32_t u = and_or<0x000F000Fu>(w >> (4 * p), magic);
+      const __nv_bfloat162 h = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&u), __floats2bfloat162_rn(136.f, 136.f));
+      r[p] = *reinterpret_cast<const uint32_t*>(&h);
     }
   } else {
     // sign | e e m at bits 15 and 11..9 of f16 (subnormals included) is 2^-14 times the e2m1 value.  The packed halves
@@ -83,20 +78,28 @@ __device__ __forceinline__ void decode(uint32_t w, uint32_t magic, uint32_t (&r)
   }
 }
 
-__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                         uint32_t b1) {
-  asm(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+template <int FMT>
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (FMT == kInt4)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-
 // the same with a zero accumulator
-__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                              uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+template <int FMT>
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (FMT == kInt4)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // GB: 32-k blocks per scale (1, 2, 4); MXFP4 has one byte per block.
@@ -119,6 +122,30 @@ struct Scales {
   }
 };
 
+// Stage columns [c0, c0 + cols) (cols a multiple of 128, columns from K on as zero) of rows [0, rows) of x as they are.
+__device__ __forceinline__ void stage_bf16(const Args& a, const __nv_bfloat16* x, int rows, uint32_t dst, int c0, int cols) {
+  const int warps = blockDim.x >> 5, lane = threadIdx.x & 31, per = (cols + 255) >> 8;  // 256 columns a warp and step
+  for (int i = threadIdx.x >> 5, r = 0; r < rows; i += warps) {
+    while (i >= per) { i -= per; ++r; }
+    if (r >= rows) break;
+    const int c = i * 256 + lane * 8;
+    if (c >= cols) continue;
+    const uint32_t to = dst + (uint32_t)r * a.x_pitch + c * 2;
+    const __nv_bfloat16* from = x + (long long)r * a.x_stride + c0 + c;
+    if (c0 + c >= a.K) {  // K is a multiple of 32: a piece of 8 lies inside or outside
+      asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
+    } else if (a.x_vec) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    } else {
+      uint32_t u[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        u[j] = (uint32_t)__bfloat16_as_ushort(from[2 * j]) | ((uint32_t)__bfloat16_as_ushort(from[2 * j + 1]) << 16);
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]) : "memory");
+    }
+  }
+}
+
 // Stage columns [c0, c0 + cols) (cols a multiple of 128, columns from K on as zero) of rows [0, rows) of x as f16, and
 // per chunk and row the power of two that undoes the scaling (bf16).  16 lanes own a row's chunk, 8 columns each.
 template <int NT>
@@ -126,7 +153,7 @@ __device__ __forceinline__ void stage_x(const Args& a, const __nv_bfloat16* x, i
   const int lane = threadIdx.x & 31, half = threadIdx.x >> 4, halves = blockDim.x >> 4;
   const uint32_t lanes = 0xffffu << (lane & 16);
   const int chunks = cols >> 7;
-  constexpr int kBatch = NT == 1 ? 4 : 8;  // loads in flight per thread
+  constexpr int kBatch = 8;  // loads in flight per thread
   int r = 0, ch = half;
   while (ch >= chunks) { ch -= chunks; ++r; }
   while (r < rows) {
@@ -185,7 +212,7 @@ __device__ __forceinline__ void stage_x(const Args& a, const __nv_bfloat16* x, i
   }
 }
 
-// CTA: blockDim / 32 warps = rw x kw; the kw warps of a tile take consecutive parts of its K.  Tiles go round all
+// CTA: 16 warps = rw x kw; the kw warps of a tile take consecutive parts of its K.  Tiles go round all
 // CTAs first, then over a CTA's rw rows of warps, so that a last incomplete round leaves every SM the same work.  The
 // sums of the kw warps meet in shared memory, in warp order.  Rows of x beyond 8 NT are the business of other blockIdx.y.
 //
@@ -200,14 +227,14 @@ __global__ void __launch_bounds__(512, 1) linear_w4_kernel(const Args a) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   using Sc = Scales<FMT, GB>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int warps = blockDim.x >> 5, kw_n = a.kw, rw_n = warps / kw_n;
-  const int wk = warp % kw_n, wr = warp / kw_n;
+  const int kw_n = 1 << a.kw_log2, rw_log2 = 4 - a.kw_log2, rw_n = 1 << rw_log2;
+  const int wk = warp & (kw_n - 1), wr = warp >> a.kw_log2;
   const int row0 = blockIdx.y * (8 * NT), rows = min(a.n - row0, 8 * NT);
   const __nv_bfloat16* x = a.x + (long long)row0 * a.x_stride;
   const int n_tiles = (a.N + kTileRows - 1) / kTileRows;
   const int tile0 = wr * (int)gridDim.x + (int)blockIdx.x, tile_step = rw_n * (int)gridDim.x;
   const int n_phases = WHOLE ? 1 : (a.n_chunks + a.phase_chunks - 1) / a.phase_chunks;
-  const int items = a.phase_chunks / kw_n;           // chunks of a warp per segment, at most
+  const int items = a.phase_chunks >> a.kw_log2;           // chunks of a warp per segment, at most
   const int blocks = (items + kDepth - 1) / kDepth;  // the same for every warp and segment
   // a piece of x: rows, then its scales [chunk][8 NT]
   const uint32_t buf_bytes = a.buf_bytes;
@@ -264,21 +291,26 @@ __global__ void __launch_bounds__(512, 1) linear_w4_kernel(const Args a) {
     if (s_left > 0) {
       const int c0 = s_phase * a.phase_chunks;
       uint8_t* to = smem + s_buf * buf_bytes;
-      stage_x<NT>(a, x, rows, to, reinterpret_cast<uint16_t*>(to + (size_t)rows * a.x_pitch), c0 * kChunk, min(a.phase_chunks, a.n_chunks - c0) * kChunk);
+      if constexpr (FMT == kInt4) stage_bf16(a, x, rows, (uint32_t)__cvta_generic_to_shared(to), c0 * kChunk, min(a.phase_chunks, a.n_chunks - c0) * kChunk);
+      else stage_x<NT>(a, x, rows, to, reinterpret_cast<uint16_t*>(to + (size_t)rows * a.x_pitch), c0 * kChunk, min(a.phase_chunks, a.n_chunks - c0) * kChunk);
       --s_left;
       s_phase = s_phase + 1 == n_phases ? 0 : s_phase + 1;
       s_buf ^= 1;
     }
   };
+  auto landed = [&] {
+    if constexpr (FMT == kInt4) asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+  };
   stage();
-  if (WHOLE) __syncthreads();
+  if (WHOLE) landed();
   // this lane's rows of x (rows that are not there read another one's: their columns of the product are not used) and
   // the scales of tokens 2 t and 2 t + 1
   uint32_t xoff[NT];
 #pragma unroll
   for (int q = 0; q < NT; ++q) xoff[q] = (uint32_t)min(q * 8 + g, rows - 1) * a.x_pitch + t * 16;
   const uint32_t boff = (uint32_t)rows * a.x_pitch + t * 4;
-  uint32_t magic = 0x64006400u;
+  uint32_t magic = 0x43004300u;
   asm volatile("" : "+r"(magic));  // in a register, so that mask and or are one instruction
 
   int buf = 1;
@@ -287,7 +319,7 @@ __global__ void __launch_bounds__(512, 1) linear_w4_kernel(const Args a) {
     float acc[NT][4] = {};
     for (int phase = 0; phase < n_phases; ++phase) {
       if (!WHOLE) {
-        __syncthreads();  // the piece is there, and everybody has left the other buffer
+        landed();  // the piece is there, and everybody has left the other buffer
         stage();
         buf ^= 1;
       }
@@ -302,7 +334,7 @@ __global__ void __launch_bounds__(512, 1) linear_w4_kernel(const Args a) {
           if (d < left) {
             const uint32_t word[8] = {wreg[d][0].x, wreg[d][0].y, wreg[d][0].z, wreg[d][0].w,
                                       wreg[d][1].x, wreg[d][1].y, wreg[d][1].z, wreg[d][1].w};
-            float part[NT][4];  // the chunk's sums, in units of its tokens' powers of two
+            float part[NT][4];  // MXFP4: the chunk's sums, in units of its tokens' powers of two
 #pragma unroll
             for (int gr = 0; gr < 4 / GB; ++gr) {
               float sum[NT][4];
@@ -315,9 +347,9 @@ __global__ void __launch_bounds__(512, 1) linear_w4_kernel(const Args a) {
 #pragma unroll
                 for (int q = 0; q < NT; ++q) {
                   const uint4 xb = *reinterpret_cast<const uint4*>(xp[q] + d * (kChunk * 2) + b * 64);
-                  if (bb == 0) mma_f16_first(sum[q], lo[0], hi[0], lo[1], hi[1], xb.x, xb.y);
-                  else mma_f16(sum[q], lo[0], hi[0], lo[1], hi[1], xb.x, xb.y);
-                  mma_f16(sum[q], lo[2], hi[2], lo[3], hi[3], xb.z, xb.w);
+                  if (bb == 0) mma_first<FMT>(sum[q], lo[0], hi[0], lo[1], hi[1], xb.x, xb.y);
+                  else mma<FMT>(sum[q], lo[0], hi[0], lo[1], hi[1], xb.x, xb.y);
+                  mma<FMT>(sum[q], lo[2], hi[2], lo[3], hi[3], xb.z, xb.w);
                 }
               }
               const float s0 = sreg[d].get(0, gr), s1 = sreg[d].get(1, gr);
@@ -325,10 +357,11 @@ __global__ void __launch_bounds__(512, 1) linear_w4_kernel(const Args a) {
               for (int q = 0; q < NT; ++q)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                  part[q][e] = gr == 0 ? (e < 2 ? s0 : s1) * sum[q][e] : fmaf(e < 2 ? s0 : s1, sum[q][e], part[q][e]);
+                  if constexpr (FMT == kInt4) acc[q][e] = fmaf(e < 2 ? s0 : s1, sum[q][e], acc[q][e]);
+                  else part[q][e] = gr == 0 ? (e < 2 ? s0 : s1) * sum[q][e] : fmaf(e < 2 ? s0 : s1, sum[q][e], part[q][e]);
             }
 #pragma unroll
-            for (int q = 0; q < NT; ++q) {
+            for (int q = 0; FMT == kMx && q < NT; ++q) {
               const uint32_t b = *reinterpret_cast<const uint32_t*>(bp + d * (16 * NT) + q * 16);
               const float f0 = __uint_as_float(b << 16), f1 = __uint_as_float(b & 0xffff0000u);
               acc[q][0] = fmaf(f0, part[q][0], acc[q][0]);
@@ -373,7 +406,7 @@ __global__ void __launch_bounds__(512, 1) linear_w4_kernel(const Args a) {
         for (int e = 0; e < 4; ++e) mine[(q * 8 + 2 * t + (e & 1)) * kRedPitch + g + 8 * (e >> 1)] = acc[q][e];
       __syncthreads();
       for (int z = threadIdx.x; z < rw_n * kTileRows * rows; z += blockDim.x) {
-        const int lo = z & 15, rr = z >> 4, w = rr % rw_n, r = rr / rw_n;
+        const int lo = z & 15, rr = z >> 4, w = rr & (rw_n - 1), r = rr >> rw_log2;
         const int o = ((round * rw_n + w) * (int)gridDim.x + (int)blockIdx.x) * kTileRows + lo;
         if (o < a.N) {
           const float* p = red + w * kw_n * (NT * 8 * kRedPitch) + r * kRedPitch + lo;
