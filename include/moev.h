@@ -354,7 +354,7 @@ typedef struct {
   const void* residual;    /* [n, H] or NULL = 0 */
   const void* w;           /* [H] */
   void* residual_out;      /* [n, H] or NULL */
-  void* y;                 /* [n, H]; NULL allowed when codes are wanted only */
+  void* y;                 /* [n, H] or NULL; one of residual_out, y and codes is given */
   uint8_t* codes;          /* [n, H] e4m3 or NULL */
   float* scales;           /* [n, ceil(H / 128)] or NULL */
   int64_t x_stride, residual_stride, residual_out_stride, y_stride, codes_stride;
@@ -426,6 +426,43 @@ size_t moev_cache_attend_workspace(const moev_kv_cache* cache, const moev_draft_
 moev_status moev_cache_attend(const moev_kv_cache* cache, const moev_draft_batch* batch, const void* q, int64_t q_stride,
                               int32_t n_heads, float scale, int32_t window, const float* sinks, void* out,
                               int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Whole decoder blocks of a verification pass: moev_verify_chain with what stands between two MoE layers
+ * in the place of the identity.  Per block, on the residual stream h:
+ *   x = norm(h, attn_norm);  q | k | v = qkv x;  moev_cache_append;  a = moev_cache_attend;  h += o a;
+ *   x = norm(h, ffn_norm);   h += MoE(x)  (moev_verify with ctx)
+ * and after the last one, where final_norm is given, final_out = norm(h, final_norm). */
+typedef struct {
+  const void *attn_norm, *ffn_norm; /* bfloat16 [H] */
+  moev_linear qkv, o;               /* [(n_heads + 2 n_kv_heads) head_dim, H] and [H, n_heads head_dim] */
+  const void *qkv_packed, *o_packed;
+  const float *qkv_bias, *o_bias;   /* or NULL */
+  const float* sinks;               /* [n_heads] or NULL */
+  int32_t window;                   /* 0: the whole context */
+  moev_kv_cache cache;              /* the block's own */
+  moev_layer moe;
+} moev_block;
+typedef struct {
+  int32_t n_heads;
+  float eps, scale;                 /* norms; attention scores (0 = head_dim ^ -1/2) */
+  const float* rope;                /* [rope_rows, head_dim] or NULL */
+  int32_t rope_rows;
+  const void* final_norm;           /* bfloat16 [H] or NULL */
+  void* final_out;                  /* bfloat16 [batch->n_tokens, H], given exactly when final_norm is */
+} moev_block_options;
+
+/* hidden bfloat16 [batch->n_tokens, H] (contiguous): h before the first block, overwritten by h after the last.  outs[l].y
+ * receives the MoE output of block l; the other fields are diagnostics as in moev_verify.  The context is one for
+ * bfloat16 activations with max_tokens >= batch->n_tokens.  Every token row goes through the MoE layers: rows of no
+ * sequence (attention output zero) would widen the expert union.  workspace: moev_verify_blocks_workspace bytes for the
+ * same sizes (16-byte aligned, contents of no matter), one per call in flight.  blocks and outs are HOST arrays of
+ * n_blocks entries whose pointers are DEVICE pointers.  Everything but the MoE layers' own pointers (moev_verify checks those
+ * when it is their turn) is checked before the first launch.  Asynchronous on cuda_stream. */
+size_t moev_verify_blocks_workspace(const moev_ctx* ctx, int32_t n_blocks, const moev_block* blocks, const moev_draft_batch* batch,
+                                    const moev_block_options* options);
+moev_status moev_verify_blocks(moev_ctx* ctx, int32_t n_blocks, const moev_block* blocks, const moev_draft_batch* batch,
+                               const moev_block_options* options, void* hidden, const moev_out* outs, void* workspace,
+                               size_t workspace_bytes, void* cuda_stream);
 
 #ifdef __cplusplus
 }

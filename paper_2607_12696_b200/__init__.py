@@ -9,4 +9,4 @@ from .binding import (ACT_BF16, ACT_FP32, ACTQ_FP8_B128, ACTQ_FP8_B128_POW2, ACT
                       SCORE_SOFTMAX, W_BF16, W_FP32, W_FP8E4M3_B128, W_INT4, W_MXFP4, MoevConfig,
                       MoevError, MoeVerifier, expert_bytes, expert_code_bytes, lib, lib_path,
                       route_topk_static, select_drafts, static_scratch_floats)
-from .block import DraftBatch, KvCache, W4Linear, add_rmsnorm, cache_append, cache_attend, cache_attend_workspace  # noqa: F401
+from .block import Block, DraftBatch, KvCache, W4Linear, add_rmsnorm, cache_append, cache_attend, cache_attend_workspace  # noqa: F401

@@ -23,7 +23,7 @@ EXPORTS = ("moev_create", "moev_destroy", "moev_verify", "moev_verify_host", "mo
            "moev_profile_read", "moev_route_topk_static", "moev_route_topk_static_scratch_floats", "moev_select_drafts",
            "moev_verify_pipeline", "moev_prefetch_enable", "moev_verify_chain", "moev_ffn_span_enable",
            "moev_ffn_span_read", "moev_add_rmsnorm", "moev_w4_packed_bytes", "moev_w4_pack", "moev_linear_w4", "moev_cache_append",
-           "moev_cache_attend_workspace", "moev_cache_attend")
+           "moev_cache_attend_workspace", "moev_cache_attend", "moev_verify_blocks_workspace", "moev_verify_blocks")
 
 
 class MoevError(RuntimeError):
@@ -75,6 +75,17 @@ class _KvCache(C.Structure):
 class _DraftBatch(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_seq", "n_tokens", "max_drafts", "max_len", "table_cols")] + \
                [(n, C.c_void_p) for n in ("cu", "ctx_len", "page_table", "parent", "status")]
+
+
+class _Block(C.Structure):
+    _fields_ = [("attn_norm", C.c_void_p), ("ffn_norm", C.c_void_p), ("qkv", _Linear), ("o", _Linear)] + \
+               [(n, C.c_void_p) for n in ("qkv_packed", "o_packed", "qkv_bias", "o_bias", "sinks")] + \
+               [("window", C.c_int32), ("cache", _KvCache), ("moe", _Layer)]
+
+
+class _BlockOptions(C.Structure):
+    _fields_ = [("n_heads", C.c_int32), ("eps", C.c_float), ("scale", C.c_float), ("rope", C.c_void_p), ("rope_rows", C.c_int32),
+                ("final_norm", C.c_void_p), ("final_out", C.c_void_p)]
 
 
 @dataclass
@@ -179,6 +190,11 @@ def lib() -> C.CDLL:
         L.moev_cache_attend.restype = C.c_int
         L.moev_cache_attend.argtypes = [C.POINTER(_KvCache), C.POINTER(_DraftBatch), vp, i64, i32, C.c_float, i32, vp, vp, i64, vp, vp,
                                         C.c_size_t, vp]
+        blocks = [vp, i32, C.POINTER(_Block), C.POINTER(_DraftBatch), C.POINTER(_BlockOptions)]
+        L.moev_verify_blocks_workspace.restype = C.c_size_t
+        L.moev_verify_blocks_workspace.argtypes = blocks
+        L.moev_verify_blocks.restype = C.c_int
+        L.moev_verify_blocks.argtypes = blocks + [vp, C.POINTER(_Out), vp, C.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -329,6 +345,11 @@ class MoeVerifier:
             for f in _OUT_FIELDS:
                 setattr(OA[i], f, _ptr(out.get(f)))
         self._check(lib().moev_verify_chain(self._h, n, LA, _ptr(x0), gamma, OA, self._stream()))
+
+    def verify_blocks(self, blocks: list, batch, hidden: torch.Tensor, n_heads: int, outs: list, **options):
+        """moev_verify_blocks: whole decoder blocks (:class:`paper_2607_12696_b200.Block`); see ``block.verify_blocks``."""
+        from .block import verify_blocks
+        return verify_blocks(self, blocks, batch, hidden, n_heads, outs, **options)
 
     def verify_host(self, layer: _Layer, x_host: torch.Tensor, gamma: int, y_host: torch.Tensor,
                     n_active_host: torch.Tensor):

@@ -8,10 +8,12 @@ whose tensors do not fit raises :class:`MoevError` (``MOEV_EINVAL``) before anyt
 from __future__ import annotations
 
 import ctypes as C
+from dataclasses import dataclass
 
 import torch
 
-from .binding import ACTQ_NONE, W_INT4, W_MXFP4, MoevError, _DraftBatch, _KvCache, _Linear, lib
+from .binding import (_OUT_FIELDS, ACTQ_NONE, W_INT4, W_MXFP4, MoevError, _Block, _BlockOptions, _DraftBatch, _KvCache, _Layer, _Linear, _Out, _ptr,
+                      lib)
 
 _EINVAL = 1
 _ext = None
@@ -166,3 +168,70 @@ def cache_attend(cache: KvCache, batch: DraftBatch, q: torch.Tensor, out: torch.
     elif scale == 0.0:
         _bad("scale: expected a positive number")
     return (_ext or _fast()).cache_attend(cache._at, batch._at, batch._parents, cache._dev, q, out, lse, scale, window, sinks, workspace)
+
+
+@dataclass
+class Block:
+    """One decoder block for :meth:`MoeVerifier.verify_blocks`: norm weights bfloat16 [H], the fused query / key / value
+    projection and the output projection, the block's cache, its MoE layer (``binding.make_layer``)."""
+    attn_norm: torch.Tensor
+    qkv: W4Linear
+    o: W4Linear
+    cache: KvCache
+    ffn_norm: torch.Tensor
+    layer: _Layer
+    window: int = 0
+    sinks: torch.Tensor = None
+
+    def _c(self, H: int, n_heads: int) -> _Block:
+        for name, t in (("attn_norm", self.attn_norm), ("ffn_norm", self.ffn_norm)):
+            if t.dtype != torch.bfloat16 or t.shape != (H,) or not t.is_contiguous():
+                _bad(f"{name}: expected {H} contiguous bfloat16 values")
+        if self.sinks is not None and (self.sinks.dtype != torch.float32 or self.sinks.shape != (n_heads,) or not self.sinks.is_contiguous()):
+            _bad(f"sinks: expected contiguous float32 [{n_heads}]")
+        return _Block(self.attn_norm.data_ptr(), self.ffn_norm.data_ptr(), self.qkv._c, self.o._c, self.qkv._args[1], self.o._args[1],
+                      self.qkv._args[2], self.o._args[2], _ptr(self.sinks), self.window, self.cache._c, self.layer)
+
+
+def verify_blocks(verifier, blocks: list, batch: DraftBatch, hidden: torch.Tensor, n_heads: int, outs: list, rope: torch.Tensor = None,
+                  eps: float = 1e-6, scale: float = None, final_norm: torch.Tensor = None, final_out: torch.Tensor = None,
+                  workspace: torch.Tensor = None):
+    """moev_verify_blocks: ``hidden`` bfloat16 [n_tokens, H] is the residual stream before the first block and becomes the one
+    after the last; ``outs[l]`` (``MoeVerifier.alloc_out``) receives block l's MoE outputs; with ``final_norm`` the normed
+    stream goes to ``final_out``.  Returns the workspace, which a next call of the same size may be given."""
+    H = verifier.cfg.H
+    if hidden.dtype != torch.bfloat16 or hidden.dim() != 2 or hidden.shape[1] != H or not hidden.is_contiguous():
+        _bad(f"hidden: expected contiguous bfloat16 [n_tokens, {H}], got {tuple(hidden.shape)} {hidden.dtype}")
+    T, n = hidden.shape[0], len(blocks)
+    if len(outs) != n or not n:
+        _bad(f"{n} blocks and {len(outs)} outputs")
+    if batch.parent is not None and batch._parents < T:
+        _bad(f"parent has {batch._parents} entries for {T} token rows")
+    D = blocks[0].cache.head_dim
+    if rope is not None and (rope.dtype != torch.float32 or rope.dim() != 2 or rope.shape[1] != D or not rope.is_contiguous()):
+        _bad(f"rope: expected contiguous float32 [positions, {D}]")
+    if any(b.cache.head_dim != D for b in blocks):
+        _bad("blocks with heads of different sizes need a call each")
+    if (final_norm is None) != (final_out is None):
+        _bad("final_norm and final_out go together")
+    if final_norm is not None and (final_norm.dtype != torch.bfloat16 or final_norm.shape != (H,) or not final_norm.is_contiguous()
+                                   or final_out.dtype != torch.bfloat16 or final_out.shape != (T, H) or not final_out.is_contiguous()):
+        _bad(f"final_norm, final_out: expected contiguous bfloat16 [{H}] and [{T}, {H}]")
+    _same_device(hidden, batch.cu, rope, final_norm, final_out, workspace, *[t for b in blocks for t in (b.cache.k, b.attn_norm, b.qkv.packed, b.o.packed)],
+                 *[o["y"] for o in outs])
+    for o in outs:
+        if o["y"].dtype != torch.bfloat16 or o["y"].shape[0] < T or o["y"].shape[1:] != (H,) or not o["y"].is_contiguous():
+            _bad(f"outs: y must be contiguous bfloat16 [{T}, {H}]")
+    BA = (_Block * n)(*[b._c(H, n_heads) for b in blocks])
+    OA = (_Out * n)()
+    for i, out in enumerate(outs):
+        for f in _OUT_FIELDS:
+            setattr(OA[i], f, _ptr(out.get(f)))
+    d = _DraftBatch.from_buffer_copy(batch._c)
+    d.n_tokens = T
+    opt = _BlockOptions(n_heads, eps, 0.0 if scale is None else scale, _ptr(rope), 0 if rope is None else rope.shape[0], _ptr(final_norm), _ptr(final_out))
+    size = lib().moev_verify_blocks_workspace(verifier._h, n, BA, C.byref(d), C.byref(opt))
+    if size and (workspace is None or workspace.numel() * workspace.element_size() < size):
+        workspace = torch.empty(size, dtype=torch.uint8, device=hidden.device)
+    verifier._check(lib().moev_verify_blocks(verifier._h, n, BA, C.byref(d), C.byref(opt), hidden.data_ptr(), OA, _ptr(workspace), size, verifier._stream()))
+    return workspace

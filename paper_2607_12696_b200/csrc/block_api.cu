@@ -1,6 +1,7 @@
 // Host side of the operators around the MoE layer (the second part of include/moev.h): argument
 // checks, launch rules, launches.  Stateless: no context, nothing allocated, nothing kept.
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 
 #include "attend.cuh"
@@ -8,6 +9,11 @@
 #include "kv_cache.cuh"
 #include "linear_w4.cuh"
 #include "norm.cuh"
+
+namespace moev {  // moev_api.cu
+const moev_config& ctx_config(const moev_ctx* c);
+moev_status ctx_fail(moev_ctx* c, moev_status st, const char* text);
+}  // namespace moev
 
 using namespace moev;
 
@@ -234,7 +240,7 @@ moev_status moev_add_rmsnorm(const moev_norm* p, void* cuda_stream) {
   if (!p || p->n < 0 || p->H < 1 || p->H > 32768 || p->afmt < 0 || p->afmt > MOEV_ACT_BF16 || p->wfmt < 0 || p->wfmt > MOEV_ACT_BF16)
     return MOEV_EINVAL;
   if (p->act_quant < 0 || p->act_quant > MOEV_ACTQ_FP8_B128_POW2 || !(p->eps >= 0.f)) return MOEV_EINVAL;
-  if (!p->x || !p->w || (!p->y && !p->codes) || (p->act_quant != 0) != (p->codes != nullptr) || (p->codes != nullptr) != (p->scales != nullptr))
+  if (!p->x || !p->w || (!p->y && !p->codes && !p->residual_out) || (p->act_quant != 0) != (p->codes != nullptr) || (p->codes != nullptr) != (p->scales != nullptr))
     return MOEV_EINVAL;
   const int es = p->afmt == MOEV_ACT_BF16 ? 2 : 4, ws = p->wfmt == MOEV_ACT_BF16 ? 2 : 4;
   bool vec = p->H % 8 == 0 && aligned(p->w, 16) && aligned(p->codes, 8) && (!p->codes || p->codes_stride % 8 == 0);
@@ -385,6 +391,119 @@ moev_status moev_cache_attend(const moev_kv_cache* c, const moev_draft_batch* d,
   a.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   return done(c->head_dim == 64 ? launch_attend_d<64>(a, p.rows, st) : launch_attend_d<128>(a, p.rows, st));
+}
+
+
+namespace {
+struct BlockBuffers {  // byte offsets in the workspace
+  size_t x, qkv, attn, o, attend, total;
+};
+BlockBuffers block_buffers(const moev_config& g, int n_blocks, const moev_block* blocks, const moev_draft_batch* d, int n_heads) {
+  auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
+  size_t qkv = 0, attn = 0, att_ws = 0;
+  const size_t T = d->n_tokens;
+  for (int l = 0; l < n_blocks; ++l) {
+    const moev_kv_cache& c = blocks[l].cache;
+    qkv = std::max(qkv, T * (size_t)(n_heads + 2 * c.n_kv_heads) * c.head_dim * 2);
+    attn = std::max(attn, T * (size_t)n_heads * c.head_dim * 2);
+    att_ws = std::max(att_ws, moev_cache_attend_workspace(&c, d, n_heads, blocks[l].window));
+  }
+  BlockBuffers b;
+  b.x = 0;
+  b.qkv = b.x + up(T * g.H * 2);
+  b.attn = b.qkv + up(qkv);
+  b.o = b.attn + up(attn);
+  b.attend = b.o + up(T * g.H * 2);
+  b.total = b.attend + up(att_ws);
+  return b;
+}
+// what is wrong with the call, or null
+const char* blocks_refuse(const moev_config& g, int n_blocks, const moev_block* blocks, const moev_draft_batch* d, const moev_block_options* o) {
+  if (n_blocks < 1 || !blocks || !d || !o) return "no blocks, batch or options";
+  if (g.afmt != MOEV_ACT_BF16) return "decoder blocks need a context for bfloat16 activations";
+  if (d->n_tokens < 1 || d->n_tokens > g.max_tokens) return "n_tokens must be in 1..max_tokens of the context";
+  if (!(o->eps >= 0.f) || !(o->scale >= 0.f)) return "eps and scale must not be negative";
+  if ((o->final_norm != nullptr) != (o->final_out != nullptr) || !aligned(o->final_norm, 16) || !aligned(o->final_out, 16)) return "final_norm and final_out go together, 16-byte aligned";
+  if (o->rope && (o->rope_rows < 1 || !aligned(o->rope, 16))) return "rope needs rows and 16-byte alignment";
+  for (int l = 0; l < n_blocks; ++l) {
+    const moev_block& b = blocks[l];
+    if (!batch_ok(&b.cache, d)) return "a block's cache or the batch is invalid";
+    if (o->n_heads < 1 || o->n_heads % b.cache.n_kv_heads) return "n_heads must be a multiple of n_kv_heads";
+    const int64_t row = (int64_t)o->n_heads * b.cache.head_dim, all = row + 2 * (int64_t)b.cache.n_kv_heads * b.cache.head_dim;
+    if (!linear_ok(&b.qkv) || !linear_ok(&b.o) || b.qkv.K != g.H || b.qkv.N != all || b.o.K != row || b.o.N != g.H)
+      return "qkv must be [(n_heads + 2 n_kv_heads) head_dim, H] and o [H, n_heads head_dim]";
+    if (!b.attn_norm || !b.ffn_norm || !b.qkv_packed || !b.o_packed || !aligned(b.attn_norm, 16) || !aligned(b.ffn_norm, 16) ||
+        !aligned(b.qkv_packed, 16) || !aligned(b.o_packed, 16) || !aligned(b.qkv_bias, 4) || !aligned(b.o_bias, 4) || !aligned(b.sinks, 4))
+      return "a block's norm or projection weight is null or misaligned";
+    if (b.window < 0) return "window must not be negative";
+  }
+  return nullptr;
+}
+}  // namespace
+
+size_t moev_verify_blocks_workspace(const moev_ctx* ctx, int32_t n_blocks, const moev_block* blocks, const moev_draft_batch* d,
+                                    const moev_block_options* o) {
+  if (!ctx || blocks_refuse(ctx_config(ctx), n_blocks, blocks, d, o)) return 0;
+  return block_buffers(ctx_config(ctx), n_blocks, blocks, d, o->n_heads).total;
+}
+
+moev_status moev_verify_blocks(moev_ctx* ctx, int32_t n_blocks, const moev_block* blocks, const moev_draft_batch* d, const moev_block_options* o,
+                               void* hidden, const moev_out* outs, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (!ctx) return MOEV_EINVAL;
+  const moev_config& g = ctx_config(ctx);
+  if (const char* why = blocks_refuse(g, n_blocks, blocks, d, o)) return ctx_fail(ctx, MOEV_EINVAL, why);
+  if (!hidden || !aligned(hidden, 16) || !outs) return ctx_fail(ctx, MOEV_EINVAL, "hidden or outs is null or misaligned");
+  for (int l = 0; l < n_blocks; ++l)
+    if (!outs[l].y || !aligned(outs[l].y, 16) || !outs[l].n_active) return ctx_fail(ctx, MOEV_EINVAL, "every block needs outs[l].y (16-byte aligned) and n_active");
+  const BlockBuffers w = block_buffers(g, n_blocks, blocks, d, o->n_heads);
+  if (!workspace || !aligned(workspace, 16) || workspace_bytes < w.total) return ctx_fail(ctx, MOEV_EINVAL, "workspace too small or misaligned");
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const int T = d->n_tokens, H = g.H;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  moev_norm n{};
+  n.n = T;
+  n.H = H;
+  n.afmt = n.wfmt = MOEV_ACT_BF16;
+  n.eps = o->eps;
+  n.x_stride = n.residual_stride = n.residual_out_stride = n.y_stride = H;
+#define STEP(call, text)                                    \
+  do {                                                      \
+    const moev_status r = (call);                           \
+    if (r != MOEV_OK) return ctx_fail(ctx, r, text);        \
+  } while (0)
+  for (int l = 0; l < n_blocks; ++l) {
+    const moev_block& b = blocks[l];
+    const int D = b.cache.head_dim;
+    const int64_t row = (int64_t)o->n_heads * D, kv_row = (int64_t)b.cache.n_kv_heads * D, all = row + 2 * kv_row;
+    uint16_t* qkv = reinterpret_cast<uint16_t*>(ws + w.qkv);
+    // h += MoE output of the block before, in the norm's pass over it
+    n.w = b.attn_norm;
+    n.y = ws + w.x;
+    n.x = l ? outs[l - 1].y : hidden;
+    n.residual = l ? hidden : nullptr;
+    n.residual_out = l ? hidden : nullptr;
+    STEP(moev_add_rmsnorm(&n, st), "attention norm");
+    STEP(moev_linear_w4(&b.qkv, b.qkv_packed, b.qkv_bias, ws + w.x, H, T, qkv, all, MOEV_ACT_BF16, st), "qkv projection");
+    STEP(moev_cache_append(&b.cache, d, qkv + row, all, qkv + row + kv_row, all, o->rope, o->rope_rows, qkv, all, o->n_heads, qkv, all, st), "cache append");
+    if (cudaMemsetAsync(ws + w.attn, 0, (size_t)T * row * 2, st) != cudaSuccess) return ctx_fail(ctx, MOEV_ECUDA, "memset failed");
+    STEP(moev_cache_attend(&b.cache, d, qkv, all, o->n_heads, o->scale > 0.f ? o->scale : (float)(1.0 / std::sqrt((double)D)), b.window, b.sinks,
+                           ws + w.attn, row, nullptr, ws + w.attend, w.total - w.attend, st),
+         "attention");
+    STEP(moev_linear_w4(&b.o, b.o_packed, b.o_bias, ws + w.attn, row, T, ws + w.o, H, MOEV_ACT_BF16, st), "output projection");
+    n.w = b.ffn_norm;
+    n.x = ws + w.o;
+    n.residual = n.residual_out = hidden;
+    STEP(moev_add_rmsnorm(&n, st), "MoE norm");
+    const moev_status r = moev_verify(ctx, &b.moe, ws + w.x, T, &outs[l], st);
+    if (r != MOEV_OK) return r;
+  }
+  n.x = outs[n_blocks - 1].y;
+  n.residual = n.residual_out = hidden;
+  n.w = o->final_norm ? o->final_norm : blocks[n_blocks - 1].ffn_norm;
+  n.y = o->final_out;
+  STEP(moev_add_rmsnorm(&n, st), "final norm");
+#undef STEP
+  return MOEV_OK;
 }
 
 }  // extern "C"

@@ -382,6 +382,12 @@ void launch_simt_ffn_w(moev_ctx* c, const LayerPtrs& L, const void* x, int gamma
 
 }  // namespace
 
+// for the other translation unit of the library (block_api.cu)
+namespace moev {
+__attribute__((visibility("hidden"))) const moev_config& ctx_config(const moev_ctx* c) { return c->cfg; }
+__attribute__((visibility("hidden"))) moev_status ctx_fail(moev_ctx* c, moev_status st, const char* text) { return fail(c, st, "%s", text); }
+}  // namespace moev
+
 extern "C" {
 
 size_t moev_expert_code_bytes(const moev_config* cfg) { return cfg ? code_bytes(cfg) : 0; }
