@@ -213,7 +213,24 @@ __device__ __forceinline__ Extent extent(const Args& a, const Seq& s, int R) {
   }
   return e;
 }
+// How the line of units is cut: units per segment and per CTA.  A CTA that goes on in another segment sets up anew, which costs
+// it as much as about 8 tiles; so where one sequence's segments can each have CTAs of their own and no run gets longer by
+// more than that, every segment is padded to whole runs (128 drafts x heads over 16 000 keys: 104 us against 124).
+struct Cut {
+  int unit, per;
+  bool own;  // runs do not go on
+};
 __device__ __forceinline__ int units_per_cta(int total, int grid) { return max(1, (int)(((unsigned)total + grid - 1) / (unsigned)grid)); }
+
+__device__ __forceinline__ Cut cut_one(const Args& a, const Extent& e) {  // of a call with one sequence
+  const int segs = e.row_tiles * a.c.heads, even = units_per_cta(segs * e.key_tiles, a.grid);
+  Cut c{e.key_tiles, even, false};
+  if (segs > 0 && segs <= a.grid) {
+    const int per = (e.key_tiles + a.grid / segs - 1) / (a.grid / segs);
+    if (per <= even + 8) c = Cut{(e.key_tiles + per - 1) / per * per, per, true};
+  }
+  return c;
+}
 
 template <int D, int R>
 struct Cfg {
@@ -329,9 +346,11 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
   int run, run_end, seq_units, seq_segs;  // position, end; units and segments before sequence b
   int b;
   Seq s;
+  Cut cut{0, 0, false};
   {
     constexpr int kWarps = C::kThreads / 32;
-    const int each = (a.d.n_seq + C::kThreads - 1) / C::kThreads, first = tid * each, last = min(a.d.n_seq, first + each);
+    const bool few = a.d.n_seq <= 32;  // every warp then finds the same for itself, a sequence a lane
+    const int each = few ? 1 : (a.d.n_seq + C::kThreads - 1) / C::kThreads, first = few ? lane : tid * each, last = min(a.d.n_seq, first + each);
     auto weigh = [&](const Seq& q, int& units, int& segs) {
       const Extent e = extent(a, q, R);
       segs = e.row_tiles * a.c.heads;
@@ -352,26 +371,37 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
       const int u1 = __shfl_up_sync(0xffffffffu, iu, o), s1 = __shfl_up_sync(0xffffffffu, is, o);
       if (lane >= o) { iu += u1; is += s1; }
     }
-    if (lane == 31) { S.scan[0][warp] = iu; S.scan[1][warp] = is; }
-    __syncthreads();
     int total = 0, segs = 0, eu = iu - un, es = is - sg;  // eu, es: before this thread's sequences
+    if (few) {
+      total = __shfl_sync(0xffffffffu, iu, 31);
+      segs = __shfl_sync(0xffffffffu, is, 31);
+    } else {
+      if (lane == 31) { S.scan[0][warp] = iu; S.scan[1][warp] = is; }
+      __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      if (w == warp) { eu += total; es += segs; }
-      total += S.scan[0][w];
-      segs += S.scan[1][w];
+      for (int w = 0; w < kWarps; ++w) {
+        if (w == warp) { eu += total; es += segs; }
+        total += S.scan[0][w];
+        segs += S.scan[1][w];
+      }
     }
-    const int per = units_per_cta(total, a.grid);
+    int per = units_per_cta(total, a.grid);
+    if (a.d.n_seq == 1 && !a.whole) {
+      const Seq one{__shfl_sync(0xffffffffu, q.lo, 0), __shfl_sync(0xffffffffu, q.n, 0), __shfl_sync(0xffffffffu, q.ctx, 0)};
+      cut = cut_one(a, extent(a, one, R));
+      per = cut.per;
+      if (cut.own) total = segs * cut.unit;
+    }
     run = (int)min((long long)per * blockIdx.x, (long long)total);
     run_end = min(run + per, total);
-    const bool tell = blockIdx.x == 0 && !a.whole, mine = run >= eu && run < eu + un;
+    const bool tell = blockIdx.x == 0 && !a.whole && (!few || warp == 0), mine = cut.own ? lane == 0 : run >= eu && run < eu + un;
     if (tell || mine)
       for (int i = first; i < last; ++i) {
         int u, g;
         if (each > 1) q = kv::sequence(a.d, i, page);
         weigh(q, u, g);
         if (tell) a.table[i] = make_int2(eu, es);
-        if (mine && run >= eu && run < eu + u) {
+        if (mine && (cut.own || (run >= eu && run < eu + u))) {
           S.at_units = eu;
           S.at_segs = es;
           S.at_seq = i;
@@ -403,7 +433,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
   for (int piece = 0; run < run_end; ++piece) {
     Extent ext = extent(a, s, R);
     const int in_seq = run - seq_units;
-    const int unit_tiles = a.whole ? 1 : ext.key_tiles;
+    const int unit_tiles = a.whole ? 1 : cut.own ? cut.unit : ext.key_tiles;
     const int seg_in_seq = in_seq / unit_tiles, first_tile = a.whole ? 0 : in_seq - seg_in_seq * unit_tiles;
     const int head = seg_in_seq / ext.row_tiles, row0 = (seg_in_seq - head * ext.row_tiles) * R;
     const int all_tiles = ext.key_tiles, piece_tiles = a.whole ? all_tiles : min(all_tiles - first_tile, run_end - run);
@@ -705,23 +735,27 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
             }
           };
           load_scores();
-          float tmax = ok ? -INFINITY : INFINITY;
-#pragma unroll
-          for (int r = 0; r < RC; r += 2) {
-            const float4 q = *reinterpret_cast<const float4*>(&S.rcm[(r0 + rc + r) / 2][0]);
-            fma2(v[r], v[r + 1], q.x, q.y, q.z, q.w);
-            tmax = fmaxf(tmax, fmaxf(v[r], v[r + 1]));
-          }
           float& u = unit_of[rc / RC];
           const bool unit = vm > 0.f && (vm > u * kUnitUp || vm < u * kUnitDown);  // the same in the group's threads
-          if (any_of(tmax > kLimit || unit, 3 + group, 128)) {
+          bool move = it == 0;  // there is no reference yet
+          if (it > 0) {
+            float tmax = ok ? -INFINITY : INFINITY;
+#pragma unroll
+            for (int r = 0; r < RC; r += 2) {
+              const float4 q = *reinterpret_cast<const float4*>(&S.rcm[(r0 + rc + r) / 2][0]);
+              fma2(v[r], v[r + 1], q.x, q.y, q.z, q.w);
+              tmax = fmaxf(tmax, fmaxf(v[r], v[r + 1]));
+            }
+            move = any_of(tmax > kLimit || unit, 3 + group, 128);
+          }
+          if (move) {
             if (any_of(!ok, 3 + group, 128)) {  // a warp that gave up stays with the others' barriers until here: all of them leave
               leave = true;
               break;
             }
             // move the references to the maxima and the unit to the tile's largest V scale.  From the scores themselves:
             // relative to the reference of a row that has seen nothing they have lost their digits
-            load_scores();
+            if (it > 0) load_scores();
             float x[RC];
 #pragma unroll
             for (int r = 0; r < RC; ++r) x[r] = v[r] = v[r] * S.rcm[(r0 + rc + r) / 2][r & 1];
@@ -800,22 +834,31 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
               // keys behind the end or without a page count as zero, so that 0 * V is 0; a NaN of a written key goes to the
               // rows that see the key, and to no others
               const int have = S.pid[sv][seg] < 0 ? 0 : min(16, max(0, k_all - (k0 + 16 * seg)));
+              if (have < 16) {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int keep = min(4, max(0, have - 4 * e));
-                if (keep < 4) ww[e] &= keep == 0 ? 0u : 0xffffffffu >> (32 - 8 * keep);
-                const uint32_t bad = __vcmpeq4(ww[e] & 0x7f7f7f7fu, 0x7f7f7f7fu);
-                if (masked && bad) {
+                for (int e = 0; e < 4; ++e) {
+                  const int keep = min(4, max(0, have - 4 * e));
+                  ww[e] &= keep == 0 ? 0u : 0xffffffffu >> (32 - 8 * keep);
+                }
+              }
+              uint32_t any = 0;  // a byte 7f or ff carries into its top bit
+#pragma unroll
+              for (int e = 0; e < 4; ++e) any |= (ww[e] & 0x7f7f7f7fu) + 0x01010101u;
+              if (masked && (any & 0x80808080u)) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const uint32_t bad = __vcmpeq4(ww[e] & 0x7f7f7f7fu, 0x7f7f7f7fu);
                   ww[e] &= ~bad;
-                  for (int y = 0; y < 4; ++y)
-                    if ((bad >> (8 * y)) & 1u) {
-                      const int kk = seg * 16 + 4 * e + y;
-                      for (int r = 0; r < R && row0 + r < n_rows; ++r)
-                        if ((S.vis[bu][(row0 + r) / a.rep - i_first][kk >> 5] >> (kk & 31)) & 1u) {
-                          atomicOr(&S.nan_row[r][d >> 5], 1u << (d & 31));
-                          S.any_nan = 1;
-                        }
-                    }
+#pragma unroll 1
+                  for (int y = 0; y < 4 && bad; ++y) {
+                    if (!((bad >> (8 * y)) & 1u)) continue;
+                    const int kk = seg * 16 + 4 * e + y;
+                    for (int r = 0; r < R && row0 + r < n_rows; ++r)
+                      if ((S.vis[bu][(row0 + r) / a.rep - i_first][kk >> 5] >> (kk & 31)) & 1u) {
+                        atomicOr(&S.nan_row[r][d >> 5], 1u << (d & 31));
+                        S.any_nan = 1;
+                      }
+                  }
                 }
               }
             }
@@ -900,7 +943,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
     ptx::tc_fence_after();
     if (S.abort) break;
     gt += n_tiles;
-    run += a.whole ? 1 : piece_tiles;
+    run += a.whole ? 1 : cut.own ? run_end - run : piece_tiles;
     const int seq_all = ext.row_tiles * a.c.heads * (a.whole ? 1 : ext.key_tiles);
     if (run < run_end && run >= seq_units + seq_all) {  // the run goes on in another sequence
       seq_units += seq_all;
@@ -934,8 +977,10 @@ __global__ void __launch_bounds__(128) attend_combine_kernel(const Args a, const
   const Extent ext = extent(a, s, R);
   const int head = hq / a.rep, rr = i * a.rep + hq - head * a.rep;
   const int2 before = a.table[b];
-  const int per = units_per_cta(a.table[a.d.n_seq].x, a.grid);
-  const int seg = head * ext.row_tiles + rr / R, from = before.x + seg * ext.key_tiles;
+  Cut cut{ext.key_tiles, 0, false};
+  if (a.d.n_seq == 1) cut = cut_one(a, ext);
+  else cut.per = units_per_cta(a.table[a.d.n_seq].x, a.grid);
+  const int per = cut.per, seg = head * ext.row_tiles + rr / R, from = before.x + seg * cut.unit;
   const int c0 = from / per, parts = (from + ext.key_tiles - 1) / per - c0 + 1;
   if (parts == 1) return;
   const long long token = s.lo + i, at = (long long)(c0 + before.y + seg) * R + rr % R;  // row of the first part; R further on that of the next
