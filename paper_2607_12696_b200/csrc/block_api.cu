@@ -341,12 +341,12 @@ moev_status moev_cache_append(const moev_kv_cache* c, const moev_draft_batch* d,
   a.rope = rope;
   a.rope_rows = rope_rows;
   a.rep = q ? n_heads / c->n_kv_heads : 0;
-  a.q_parts = a.rep == 0 ? 0 : std::min(4, (a.rep + 1) / 2);  // a CTA each for the work of about one K and V
   // pages that max_drafts tokens can touch, wherever the first one falls in its page
   const int pages = (d->max_drafts + c->page - 2) / c->page + 1;
+  a.q_parts = std::min(2, (a.rep + 1) / 2);
   const int n_par = d->parent && rope ? std::min(d->max_drafts, kv::kMaxTree) : 0;
   const size_t smem = (size_t)(((c->page + n_par) * 4 + 15) & ~15) + (size_t)c->page * c->head_dim + (size_t)c->head_dim * (c->page + 4);
-  const dim3 grid(pages, d->n_seq, c->n_kv_heads * (1 + a.q_parts));
+  const dim3 grid(pages, c->n_kv_heads * (1 + a.q_parts), d->n_seq);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   return done(c->head_dim == 64 ? launch(kv::cache_append_kernel<64>, grid, dim3(256), smem, st, a)
                                 : launch(kv::cache_append_kernel<128>, grid, dim3(256), smem, st, a));

@@ -132,8 +132,9 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
 // One CTA per (page that a sequence's drafts touch, kv head, sequence).  The page's new rows are read
 // twice, once for the largest magnitude and once to be written, the second time from the caches; the
 // codes pass through shared memory, where those of V are turned from token rows into dimension rows.
-// Further CTAs of the page and head rotate the query heads of the group for the page's tokens, two thirds of the bytes
-// at 8 query heads a kv head.
+// Two further CTAs of the page and head rotate the query heads of the group for the page's tokens, two thirds of the
+// bytes at 8 query heads a kv head (in the K and V CTA itself: 64 drafts 5.1 us instead of 4.3, 5 500 tokens 44.6 instead
+// of 40.1; registers for two rows in flight cost a third of the warps and 10 us of the latter).
 // Bound by memory: 2 (Hq + 2 Hkv) D bytes in, 2 Hq D + 2 Hkv D out per token.
 template <int D>
 __global__ void __launch_bounds__(256) cache_append_kernel(const AppendArgs a) {
@@ -143,8 +144,7 @@ __global__ void __launch_bounds__(256) cache_append_kernel(const AppendArgs a) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int page = 1 << a.c.page_log2;
   // roles: K and V of a page and head (part 0), or a share of the queries of its group (parts 1 ..)
-  // The part is the slowest index: the longer K and V CTAs start first.
-  const int b = blockIdx.y, part = blockIdx.z / a.c.heads, head = blockIdx.z - part * a.c.heads, tid = threadIdx.x;
+  const int b = blockIdx.z, part = blockIdx.y / a.c.heads, head = blockIdx.y - part * a.c.heads, tid = threadIdx.x;
   const Seq s = sequence(a.d, b, page);
   const int col = (s.ctx >> a.c.page_log2) + blockIdx.x;
   const int first = max(s.ctx, col << a.c.page_log2), last = min(s.ctx + s.n, (col + 1) << a.c.page_log2);
@@ -178,28 +178,14 @@ __global__ void __launch_bounds__(256) cache_append_kernel(const AppendArgs a) {
   constexpr int kHalf = D / 16;  // pieces of 8 columns in half a row; a thread takes one and its partner
   if (part > 0) {
     const int items = m * a.rep * kHalf, step = a.q_parts * blockDim.x;
-    constexpr int kBatch = 2;  // items whose loads are in flight
-    for (int z0 = (part - 1) * blockDim.x + tid; z0 < items; z0 += kBatch * step) {
-      float x[kBatch][8], y[kBatch][8];
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const int z = z0 + k * step;
-        if (z < items) {
-          const int rr = z / kHalf, r = rr / a.rep;
-          load_rotated<D>(a.q + (s.lo + i0 + r) * a.q_stride + (head * a.rep + rr - r * a.rep) * D, a.rope ? a.rope + (long long)pos[r] * D : nullptr,
-                          (z % kHalf) * 8, x[k], y[k]);
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const int z = z0 + k * step;
-        if (z < items) {
-          const int rr = z / kHalf, r = rr / a.rep;
-          __nv_bfloat16* o = a.q_out + (s.lo + i0 + r) * a.q_out_stride + (head * a.rep + rr - r * a.rep) * D + (z % kHalf) * 8;
-          store8(o, x[k]);
-          store8(o + D / 2, y[k]);
-        }
-      }
+    for (int z = (part - 1) * blockDim.x + tid; z < items; z += step) {
+      const int rr = z / kHalf, c = (z % kHalf) * 8, r = rr / a.rep, h = head * a.rep + rr - r * a.rep;
+      const long long token = s.lo + i0 + r;
+      float x[8], y[8];
+      load_rotated<D>(a.q + token * a.q_stride + h * D, a.rope ? a.rope + (long long)pos[r] * D : nullptr, c, x, y);
+      __nv_bfloat16* o = a.q_out + token * a.q_out_stride + h * D + c;
+      store8(o, x);
+      store8(o + D / 2, y);
     }
     return;
   }
@@ -249,25 +235,12 @@ __global__ void __launch_bounds__(256) cache_append_kernel(const AppendArgs a) {
       }
       *reinterpret_cast<uint2*>(kc + r * D + c) = make_uint2(u[0], u[1]);
       *reinterpret_cast<uint2*>(kc + r * D + c + D / 2) = make_uint2(u[2], u[3]);
-    }
-    // V: a thread takes four neighbouring slots and 8 dimensions, and writes words of four tokens.  Of 32 lanes 8 are
-    // neighbours in the slots and 4 in the dimensions: 64-byte runs of global memory, 32 banks of shared memory.
-    const int g0 = fill >> 2, groups = ((fill + m + 3) >> 2) - g0;
-    for (int z = tid; z < ((groups + 7) & ~7) * (D / 8); z += blockDim.x) {
-      const int block = z >> 5, g = (block / (D / 32)) * 8 + (z & 7), c = ((block % (D / 32)) * 4 + ((z >> 3) & 3)) * 8;
-      if (g >= groups) continue;
-      uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      load_rotated<D>(vrow + (long long)r * a.v_stride, nullptr, c, x, y);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int r = 4 * (g0 + g) + k - fill;
-        if (r < 0 || r >= m) continue;
-        float x[8];
-        load8(vrow + (long long)r * a.v_stride + c, x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] |= cache_code(x[i], v_inv) << (8 * k);
+      for (int i = 0; i < 8; ++i) {
+        vc[(c + i) * v_pitch + fill + r] = (uint8_t)cache_code(x[i], v_inv);
+        vc[(c + i + D / 2) * v_pitch + fill + r] = (uint8_t)cache_code(y[i], v_inv);
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) *reinterpret_cast<uint32_t*>(vc + (c + i) * v_pitch + 4 * (g0 + g)) = w[i];
     }
     __syncthreads();
     // K: the new rows are one contiguous run; the kept rows only where the scale grew
