@@ -60,14 +60,15 @@ moev_status done(cudaError_t e) {
 // ---------------------------------------------------------------- norm
 template <typename T, typename TW, bool VEC>
 cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
-  // pieces of 8 columns: one per thread up to 4096 columns, else the fewest of 1, 2, 4, 8 that 512 threads can hold
+  // pieces of 8 columns: one per thread up to 8192 columns, else the fewest of 4, 8 that 512 threads can hold
   const int pieces = (a.H + 7) / 8;
-  const int pv = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : pieces <= 2048 ? 4 : 8;
+  const int pv = pieces <= 1024 ? 1 : pieces <= 2048 ? 4 : 8;
   int threads = ((pieces + pv - 1) / pv + 31) & ~31;
-  const dim3 grid((unsigned)a.n);
+  // as many CTAs as the machine holds at 64 registers a thread, each with several rows; a row each where none is fetched ahead
+  const int resident = sm_count() * std::max(1, std::min(16, 1024 / threads));
+  const dim3 grid((unsigned)(VEC && pv == 1 ? std::min(a.n, resident) : a.n));
   switch (pv) {
     case 1: return launch(add_rmsnorm_kernel<T, TW, 1, VEC>, grid, dim3(threads), 0, st, a);
-    case 2: return launch(add_rmsnorm_kernel<T, TW, 2, VEC>, grid, dim3(threads), 0, st, a);
     case 4: return launch(add_rmsnorm_kernel<T, TW, 4, VEC>, grid, dim3(threads), 0, st, a);
     default: return launch(add_rmsnorm_kernel<T, TW, 8, VEC>, grid, dim3(threads), 0, st, a);
   }
