@@ -32,6 +32,13 @@
 // finished there; the others' parts meet in a second kernel (attend_combine), in order.  The lengths are device data,
 // so every CTA finds its run itself.  Segments of a few tiles (a window) are dealt out whole, without a second kernel.
 // Every wait is bounded.
+//
+// Bound, as measured on B200 (us; bytes at 6.5 TB/s and operations at 1.67 PFLOP/s allow the time in brackets): one draft, 16
+// rows, 4096 keys 13 (0.7): two launches, set-up, one tile and the join, each a chain of trips to memory; 64 drafts x 16
+// heads over 16 000 keys 124 (20): the softmax warps' instructions, 5 800 cycles a tile of 128 x 128, of which the tensor
+// core needs 1 800; 32 ragged sequences up to 24 000 keys, 32 rows 205 (121): 3 500 cycles a tile of 32 KB on either of an
+// SM's two CTAs, two thirds of the issue slots, 3.9 TB/s; window of 128, 64 rows, 16 sequences 16 (0.5): three masked
+// tiles a CTA.  The same work on mma.sync with the rows as the wide operand took 187 and 333 us for the second and third.
 #pragma once
 #include <cuda.h>
 
@@ -213,24 +220,7 @@ __device__ __forceinline__ Extent extent(const Args& a, const Seq& s, int R) {
   }
   return e;
 }
-// How the line of units is cut: units per segment and per CTA.  A CTA that goes on in another segment sets up anew, which costs
-// it as much as about 8 tiles; so where one sequence's segments can each have CTAs of their own and no run gets longer by
-// more than that, every segment is padded to whole runs (128 drafts x heads over 16 000 keys: 104 us against 124).
-struct Cut {
-  int unit, per;
-  bool own;  // runs do not go on
-};
 __device__ __forceinline__ int units_per_cta(int total, int grid) { return max(1, (int)(((unsigned)total + grid - 1) / (unsigned)grid)); }
-
-__device__ __forceinline__ Cut cut_one(const Args& a, const Extent& e) {  // of a call with one sequence
-  const int segs = e.row_tiles * a.c.heads, even = units_per_cta(segs * e.key_tiles, a.grid);
-  Cut c{e.key_tiles, even, false};
-  if (segs > 0 && segs <= a.grid) {
-    const int per = (e.key_tiles + a.grid / segs - 1) / (a.grid / segs);
-    if (per <= even + 8) c = Cut{(e.key_tiles + per - 1) / per * per, per, true};
-  }
-  return c;
-}
 
 template <int D, int R>
 struct Cfg {
@@ -346,7 +336,6 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
   int run, run_end, seq_units, seq_segs;  // position, end; units and segments before sequence b
   int b;
   Seq s;
-  Cut cut{0, 0, false};
   {
     constexpr int kWarps = C::kThreads / 32;
     const bool few = a.d.n_seq <= 32;  // every warp then finds the same for itself, a sequence a lane
@@ -385,23 +374,17 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         segs += S.scan[1][w];
       }
     }
-    int per = units_per_cta(total, a.grid);
-    if (a.d.n_seq == 1 && !a.whole) {
-      const Seq one{__shfl_sync(0xffffffffu, q.lo, 0), __shfl_sync(0xffffffffu, q.n, 0), __shfl_sync(0xffffffffu, q.ctx, 0)};
-      cut = cut_one(a, extent(a, one, R));
-      per = cut.per;
-      if (cut.own) total = segs * cut.unit;
-    }
+    const int per = units_per_cta(total, a.grid);
     run = (int)min((long long)per * blockIdx.x, (long long)total);
     run_end = min(run + per, total);
-    const bool tell = blockIdx.x == 0 && !a.whole && (!few || warp == 0), mine = cut.own ? lane == 0 : run >= eu && run < eu + un;
+    const bool tell = blockIdx.x == 0 && !a.whole && (!few || warp == 0), mine = run >= eu && run < eu + un;
     if (tell || mine)
       for (int i = first; i < last; ++i) {
         int u, g;
         if (each > 1) q = kv::sequence(a.d, i, page);
         weigh(q, u, g);
         if (tell) a.table[i] = make_int2(eu, es);
-        if (mine && (cut.own || (run >= eu && run < eu + u))) {
+        if (mine && run >= eu && run < eu + u) {
           S.at_units = eu;
           S.at_segs = es;
           S.at_seq = i;
@@ -433,7 +416,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
   for (int piece = 0; run < run_end; ++piece) {
     Extent ext = extent(a, s, R);
     const int in_seq = run - seq_units;
-    const int unit_tiles = a.whole ? 1 : cut.own ? cut.unit : ext.key_tiles;
+    const int unit_tiles = a.whole ? 1 : ext.key_tiles;
     const int seg_in_seq = in_seq / unit_tiles, first_tile = a.whole ? 0 : in_seq - seg_in_seq * unit_tiles;
     const int head = seg_in_seq / ext.row_tiles, row0 = (seg_in_seq - head * ext.row_tiles) * R;
     const int all_tiles = ext.key_tiles, piece_tiles = a.whole ? all_tiles : min(all_tiles - first_tile, run_end - run);
@@ -943,7 +926,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
     ptx::tc_fence_after();
     if (S.abort) break;
     gt += n_tiles;
-    run += a.whole ? 1 : cut.own ? run_end - run : piece_tiles;
+    run += a.whole ? 1 : piece_tiles;
     const int seq_all = ext.row_tiles * a.c.heads * (a.whole ? 1 : ext.key_tiles);
     if (run < run_end && run >= seq_units + seq_all) {  // the run goes on in another sequence
       seq_units += seq_all;
@@ -977,10 +960,8 @@ __global__ void __launch_bounds__(128) attend_combine_kernel(const Args a, const
   const Extent ext = extent(a, s, R);
   const int head = hq / a.rep, rr = i * a.rep + hq - head * a.rep;
   const int2 before = a.table[b];
-  Cut cut{ext.key_tiles, 0, false};
-  if (a.d.n_seq == 1) cut = cut_one(a, ext);
-  else cut.per = units_per_cta(a.table[a.d.n_seq].x, a.grid);
-  const int per = cut.per, seg = head * ext.row_tiles + rr / R, from = before.x + seg * cut.unit;
+  const int per = units_per_cta(a.table[a.d.n_seq].x, a.grid);
+  const int seg = head * ext.row_tiles + rr / R, from = before.x + seg * ext.key_tiles;
   const int c0 = from / per, parts = (from + ext.key_tiles - 1) / per - c0 + 1;
   if (parts == 1) return;
   const long long token = s.lo + i, at = (long long)(c0 + before.y + seg) * R + rr % R;  // row of the first part; R further on that of the next
