@@ -377,7 +377,7 @@ moev_status moev_linear_w4(const moev_linear* p, const void* packed, const float
                            int64_t x_stride, int32_t n, void* y, int64_t y_stride, int32_t yfmt, void* cuda_stream);
 
 /* Paged key / value cache in 8 bits.  value = code * scale, one scale per page and kv head for K and
- * one for V, a power of two wherever moev_cache_append wrote it.
+ * one for V, positive, a power of two wherever moev_cache_append wrote it.
  *   k [n_pages, n_kv_heads, page, head_dim] e4m3      v [n_pages, n_kv_heads, head_dim, page] e4m3
  *   k_scale, v_scale [n_pages, n_kv_heads] float32
  * page is 16, 32, 64 or 128, head_dim 64 or 128. */
@@ -396,8 +396,8 @@ typedef struct {
  *   max_drafts >= every sequence's drafts (<= 1024 with parents), max_len >= every ctx_len + drafts:
  * host bounds that size the launches.  The arrays are device data: a sequence that breaks the bounds is
  * left out, a page id outside the pool hides its keys, and both set *status (may be NULL; 1 sequence,
- * 2 page id, 3 position behind the rotation table; never cleared).  Rows that belong to no sequence are
- * left as they are. */
+ * 2 page id, 3 position behind the rotation table, 4 a bounded wait of the attention kernel ran out and its
+ * outputs are undefined; never cleared).  Rows that belong to no sequence are left as they are. */
 typedef struct {
   int32_t n_seq, n_tokens, max_drafts, max_len, table_cols;
   const int32_t *cu, *ctx_len, *page_table, *parent;

@@ -56,7 +56,7 @@ constexpr int kKeys = 128;                 // keys of a tile
 // p = 2^(s - m_r) may reach 2^12 and a V scale 8 times the accumulators' unit: 2^15 in f16
 constexpr float kLimit = 12.f, kUnitUp = 8.f, kUnitDown = 1.f / 64.f;
 constexpr float kUnseen = -3.0e38f;        // reference of a row that has not seen a key yet
-constexpr unsigned long long kBudgetNs = 2000000000ull;
+constexpr unsigned long long kBudgetNs = kDeviceWaitBudgetNs;  // per wait; test builds can make the last V tile stay out
 
 struct Args {
   Drafts d;
@@ -468,6 +468,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         }
         __syncwarp();
         if (on) ptx::tma_load_2d(dst, &tm_k, &S.k_full[sk], 0, (mine * a.c.heads + head) << page_log2, ptx::kPolicyEvictNormal);
+        if (MOEV_TEST_WITHHOLD() && it == n_tiles - 1) break;
         if (ct >= VS && !wait_warp(&S.v_empty[sv], ((ct / VS) & 1) ^ 1, &S.abort, a.d.status, lane)) break;
         if (lane < 8) {
           S.ks[sv][lane] = ks;

@@ -507,4 +507,12 @@ moev_status moev_verify_blocks(moev_ctx* ctx, int32_t n_blocks, const moev_block
   return MOEV_OK;
 }
 
+#ifdef MOEV_TEST_HOOKS
+// Test builds only: while the flag is set, the loader of the attention kernel leaves out the last V tile (see common.cuh).
+int32_t moev_test_withhold_attend(int32_t on) {
+  const int v = on ? 1 : 0;
+  return cudaMemcpyToSymbol(g_test_withhold, &v, sizeof(int)) == cudaSuccess ? 0 : -1;
+}
+#endif
+
 }  // extern "C"

@@ -95,8 +95,8 @@ __device__ __forceinline__ void load_rotated(const __nv_bfloat16* row, const flo
     float co[8], si[8];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float4 x = __ldg(reinterpret_cast<const float4*>(cs + c + 4 * h));
-      const float4 y = __ldg(reinterpret_cast<const float4*>(cs + D / 2 + c + 4 * h));
+      const float4 x = *reinterpret_cast<const float4*>(cs + c + 4 * h);
+      const float4 y = *reinterpret_cast<const float4*>(cs + D / 2 + c + 4 * h);
       co[4 * h] = x.x; co[4 * h + 1] = x.y; co[4 * h + 2] = x.z; co[4 * h + 3] = x.w;
       si[4 * h] = y.x; si[4 * h + 1] = y.y; si[4 * h + 2] = y.z; si[4 * h + 3] = y.w;
     }

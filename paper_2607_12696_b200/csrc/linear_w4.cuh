@@ -112,9 +112,9 @@ struct Scales {
   static constexpr int kLane = kBytes / 8;                               // per row pair: 16, 8, 4 (INT4) or 8 (MXFP4)
   uint32_t u[kLane / 4];
   __device__ __forceinline__ void load(const uint8_t* p) {
-    if constexpr (kLane == 16) { const uint4 q = __ldg(reinterpret_cast<const uint4*>(p)); u[0] = q.x; u[1] = q.y; u[2] = q.z; u[3] = q.w; }
-    else if constexpr (kLane == 8) { const uint2 q = __ldg(reinterpret_cast<const uint2*>(p)); u[0] = q.x; u[1] = q.y; }
-    else u[0] = __ldg(reinterpret_cast<const unsigned int*>(p));
+    if constexpr (kLane == 16) { const uint4 q = *reinterpret_cast<const uint4*>(p); u[0] = q.x; u[1] = q.y; u[2] = q.z; u[3] = q.w; }
+    else if constexpr (kLane == 8) { const uint2 q = *reinterpret_cast<const uint2*>(p); u[0] = q.x; u[1] = q.y; }
+    else u[0] = *reinterpret_cast<const uint32_t*>(p);
   }
   // scale of row g (half 0) or g + 8 (half 1) for the i-th group of the chunk
   __device__ __forceinline__ float get(int half, int i) const {
