@@ -217,8 +217,8 @@ def verify_blocks(verifier, blocks: list, batch: DraftBatch, hidden: torch.Tenso
     if final_norm is not None and (final_norm.dtype != torch.bfloat16 or final_norm.shape != (H,) or not final_norm.is_contiguous()
                                    or final_out.dtype != torch.bfloat16 or final_out.shape != (T, H) or not final_out.is_contiguous()):
         _bad(f"final_norm, final_out: expected contiguous bfloat16 [{H}] and [{T}, {H}]")
-    _same_device(hidden, batch.cu, rope, final_norm, final_out, workspace, *[t for b in blocks for t in (b.cache.k, b.attn_norm, b.qkv.packed, b.o.packed)],
-                 *[o["y"] for o in outs])
+    _same_device(hidden, batch.cu, rope, final_norm, final_out, workspace, *[o[f] for o in outs for f in ("y", "n_active")],
+                 *[t for b in blocks for t in (b.cache.k, b.attn_norm, b.ffn_norm, b.sinks, b.qkv.packed, b.o.packed)])
     for o in outs:
         if o["y"].dtype != torch.bfloat16 or o["y"].shape[0] < T or o["y"].shape[1:] != (H,) or not o["y"].is_contiguous():
             _bad(f"outs: y must be contiguous bfloat16 [{T}, {H}]")
@@ -231,7 +231,7 @@ def verify_blocks(verifier, blocks: list, batch: DraftBatch, hidden: torch.Tenso
     d.n_tokens = T
     opt = _BlockOptions(n_heads, eps, 0.0 if scale is None else scale, _ptr(rope), 0 if rope is None else rope.shape[0], _ptr(final_norm), _ptr(final_out))
     size = lib().moev_verify_blocks_workspace(verifier._h, n, BA, C.byref(d), C.byref(opt))
-    if size and (workspace is None or workspace.numel() * workspace.element_size() < size):
+    if size and (workspace is None or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < size):
         workspace = torch.empty(size, dtype=torch.uint8, device=hidden.device)
     verifier._check(lib().moev_verify_blocks(verifier._h, n, BA, C.byref(d), C.byref(opt), hidden.data_ptr(), OA, _ptr(workspace), size, verifier._stream()))
     return workspace

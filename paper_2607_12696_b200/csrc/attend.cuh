@@ -25,7 +25,7 @@
 //
 // Roles: one warp loads (TMA), one thread issues the MMAs, groups of four warps do the softmax of a share of the rows each
 // (tensor memory gives a warp a quarter of the lanes) and widen V.  S is double-buffered: S of tile i + 1 is computed
-// while the softmax works on tile i, the second product of tile i while it works on tile i + 1.  
+// while the softmax works on tile i, the second product of tile i while it works on tile i + 1.
 // Work split: all tiles of the call in one line (sequence, kv head, tile of rows, tile of keys), cut into equal
 // runs, one per CTA that the machine holds.  A run may end one (sequence, head, rows) segment, cover others and begin the
 // next: every CTA works equally long whatever the lengths, and sets up once or a few times.  A segment that lies in one run is

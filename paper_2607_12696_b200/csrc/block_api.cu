@@ -19,6 +19,10 @@ using namespace moev;
 
 namespace {
 
+constexpr int kMaxNorm = 32768;              // columns of a norm
+constexpr float kMaxScale = 1e6f;            // of attention scores
+constexpr long long kMaxUnits = 0x3fffffff;  // tiles of an attention call
+
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 int sm_count() {
@@ -80,7 +84,7 @@ cudaError_t launch_norm_v(const NormArgs& a, bool vec, cudaStream_t st) {
 
 // ---------------------------------------------------------------- 4-bit linear
 bool linear_ok(const moev_linear* p) {
-  if (!p || p->N < 1 || p->K < 32 || p->K % 32 || p->K > (1 << 20)) return false;
+  if (!p || p->N < 1 || p->N > (1 << 30) || p->K < 32 || p->K % 32 || p->K > (1 << 20)) return false;
   if (p->wfmt == MOEV_W_MXFP4) return p->group == 32;
   return p->wfmt == MOEV_W_INT4 && (p->group == 32 || p->group == 64 || p->group == 128) && p->K % p->group == 0;
 }
@@ -238,19 +242,19 @@ cudaError_t launch_attend_d(const att::Args& a, int rows, cudaStream_t st) {
 extern "C" {
 
 moev_status moev_add_rmsnorm(const moev_norm* p, void* cuda_stream) {
-  if (!p || p->n < 0 || p->H < 1 || p->H > 32768 || p->afmt < 0 || p->afmt > MOEV_ACT_BF16 || p->wfmt < 0 || p->wfmt > MOEV_ACT_BF16)
+  if (!p || p->n < 0 || p->H < 1 || p->H > kMaxNorm || p->afmt < 0 || p->afmt > MOEV_ACT_BF16 || p->wfmt < 0 || p->wfmt > MOEV_ACT_BF16)
     return MOEV_EINVAL;
   if (p->act_quant < 0 || p->act_quant > MOEV_ACTQ_FP8_B128_POW2 || !(p->eps >= 0.f)) return MOEV_EINVAL;
   if (!p->x || !p->w || (!p->y && !p->codes && !p->residual_out) || (p->act_quant != 0) != (p->codes != nullptr) || (p->codes != nullptr) != (p->scales != nullptr))
     return MOEV_EINVAL;
   const int es = p->afmt == MOEV_ACT_BF16 ? 2 : 4, ws = p->wfmt == MOEV_ACT_BF16 ? 2 : 4;
-  bool vec = p->H % 8 == 0 && aligned(p->w, 16) && aligned(p->codes, 8) && (!p->codes || p->codes_stride % 8 == 0);
+  bool vec = p->H % 8 == 0 && aligned(p->w, 16) && aligned(p->codes, 8) && (!p->codes || p->n == 1 || p->codes_stride % 8 == 0);
   const void* ptr[4] = {p->x, p->residual, p->y, p->residual_out};
   const int64_t stride[4] = {p->x_stride, p->residual_stride, p->y_stride, p->residual_out_stride};
   for (int i = 0; i < 4; ++i) {
     if (!ptr[i]) continue;
     if (!aligned(ptr[i], es) || (p->n > 1 && stride[i] < p->H)) return MOEV_EINVAL;
-    vec = vec && aligned(ptr[i], 16) && (stride[i] * es) % 16 == 0;
+    vec = vec && aligned(ptr[i], 16) && (p->n == 1 || (stride[i] * es) % 16 == 0);
   }
   if (!aligned(p->w, ws) || !aligned(p->scales, 4) || (p->codes && p->n > 1 && p->codes_stride < p->H)) return MOEV_EINVAL;
   if (p->n == 0) return MOEV_OK;
@@ -362,13 +366,13 @@ size_t moev_cache_attend_workspace(const moev_kv_cache* c, const moev_draft_batc
 moev_status moev_cache_attend(const moev_kv_cache* c, const moev_draft_batch* d, const void* q, int64_t q_stride, int32_t n_heads, float scale,
                               int32_t window, const float* sinks, void* out, int64_t out_stride, float* lse, void* workspace,
                               size_t workspace_bytes, void* cuda_stream) {
-  if (!batch_ok(c, d) || !q || !out || n_heads < 1 || n_heads % c->n_kv_heads || window < 0 || !(scale > 0.f) || scale > 1e6f) return MOEV_EINVAL;
+  if (!batch_ok(c, d) || !q || !out || n_heads < 1 || n_heads % c->n_kv_heads || window < 0 || !(scale > 0.f) || scale > kMaxScale) return MOEV_EINVAL;
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(sinks, 4) || q_stride % 8 || out_stride % 8) return MOEV_EINVAL;
   const int64_t row = (int64_t)n_heads * c->head_dim;
   if (d->n_tokens > 1 && (q_stride < row || out_stride < row)) return MOEV_EINVAL;
   if (d->n_seq == 0 || d->n_tokens == 0) return MOEV_OK;
   const Plan p = attend_plan(c, d, n_heads, window);
-  if ((n_heads + 3) / 4 > 65535 || p.units > 0x3fffffffLL) return MOEV_EINVAL;
+  if ((n_heads + 3) / 4 > 65535 || p.units > kMaxUnits) return MOEV_EINVAL;
   const size_t need = p.table + p.ml + p.o;
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return MOEV_EINVAL;
   att::Args a{};
@@ -423,7 +427,8 @@ const char* blocks_refuse(const moev_config& g, int n_blocks, const moev_block* 
   if (n_blocks < 1 || !blocks || !d || !o) return "no blocks, batch or options";
   if (g.afmt != MOEV_ACT_BF16) return "decoder blocks need a context for bfloat16 activations";
   if (d->n_tokens < 1 || d->n_tokens > g.max_tokens) return "n_tokens must be in 1..max_tokens of the context";
-  if (!(o->eps >= 0.f) || !(o->scale >= 0.f)) return "eps and scale must not be negative";
+  if (g.H > kMaxNorm) return "rows of more than 32768 columns are not served";
+  if (!(o->eps >= 0.f) || !(o->scale >= 0.f) || o->scale > kMaxScale) return "eps must not be negative, scale must be from 0 to 1e6";
   if ((o->final_norm != nullptr) != (o->final_out != nullptr) || !aligned(o->final_norm, 16) || !aligned(o->final_out, 16)) return "final_norm and final_out go together, 16-byte aligned";
   if (o->rope && (o->rope_rows < 1 || !aligned(o->rope, 16))) return "rope needs rows and 16-byte alignment";
   for (int l = 0; l < n_blocks; ++l) {
@@ -437,6 +442,7 @@ const char* blocks_refuse(const moev_config& g, int n_blocks, const moev_block* 
         !aligned(b.qkv_packed, 16) || !aligned(b.o_packed, 16) || !aligned(b.qkv_bias, 4) || !aligned(b.o_bias, 4) || !aligned(b.sinks, 4))
       return "a block's norm or projection weight is null or misaligned";
     if (b.window < 0) return "window must not be negative";
+    if (attend_plan(&b.cache, d, o->n_heads, b.window).units > kMaxUnits) return "the batch's bounds are too large";
   }
   return nullptr;
 }

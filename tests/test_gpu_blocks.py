@@ -177,3 +177,25 @@ def test_blocks_refuse_what_does_not_fit():
             bad()
     assert np.isfinite(m.h.float().cpu().numpy()).all()
     m.v.close()
+
+
+def test_a_refused_call_of_blocks_writes_nothing():
+    s = setup()
+    m = Model(2, s, H=704, I=320, E=32)
+    h, outs, c, b = m.h.clone(), m.outs(), m.blocks[0].cache, m.blocks[1]
+    before = [t.clone() for t in (c.k, c.v, c.k_scale, c.v_scale)]
+    other = [m.blocks[0], moev.Block(b.attn_norm, b.qkv, b.o, b.cache, b.ffn_norm.cpu(), b.layer)]
+    for bad in (lambda: m.v.verify_blocks(m.blocks, m.batch, h, m.n_heads, outs, rope=m.rope, scale=1e9),
+                lambda: m.v.verify_blocks(other, m.batch, h, m.n_heads, outs, rope=m.rope)):
+        with pytest.raises(moev.MoevError):
+            bad()
+    torch.cuda.synchronize()
+    assert torch.equal(h, m.h)
+    assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip((c.k, c.v, c.k_scale, c.v_scale), before))
+    # a workspace with gaps is not written through
+    ws = m.v.verify_blocks(m.blocks, m.batch, h, m.n_heads, outs, rope=m.rope)
+    gaps = torch.zeros(2 * ws.numel(), dtype=torch.uint8, device="cuda")[::2]
+    assert m.v.verify_blocks(m.blocks, m.batch, h, m.n_heads, outs, rope=m.rope, workspace=gaps) is not gaps
+    m.v.status_sync()
+    assert not gaps.any()
+    m.v.close()
