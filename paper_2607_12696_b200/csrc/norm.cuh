@@ -113,7 +113,8 @@ __device__ __forceinline__ void norm_unpack8(const Raw8<T>& r, float (&v)[8]) {
 // PV pieces of 8 columns per thread (H <= PV * 8 * blockDim.x); VEC: every row of every tensor starts on a
 // 16-byte (codes: 8-byte) boundary and H is a multiple of 8.  A CTA takes every gridDim.x-th row.  Where a thread has
 // one piece, rows are fetched one ahead, while the CTA waits for the sum of the one before (8192 rows of 7168 with codes:
-// a CTA of 448 threads per row 115 us, 896 threads and rows ahead 103 us, 5.1 TB/s).
+// a CTA of 448 threads per row 115 us, 896 threads and rows ahead 103 us, and with the warps' sums added across lanes and not
+// by every thread 94 us, 5.6 TB/s).
 template <typename T, typename TW, int PV, bool VEC>
 __global__ void __launch_bounds__(PV == 1 ? 1024 : 512) add_rmsnorm_kernel(NormArgs a) {
   constexpr bool kAhead = VEC && PV == 1;
@@ -181,8 +182,8 @@ __global__ void __launch_bounds__(PV == 1 ? 1024 : 512) add_rmsnorm_kernel(NormA
     ss = warp_sum(ss);
     if ((tid & 31) == 0) part[turn][tid >> 5] = ss;
     __syncthreads();  // the other half of `part` belongs to the next row
-    float tot = 0.f;
-    for (int i = 0; i < (int)(blockDim.x >> 5); ++i) tot += part[turn][i];  // same order in every thread
+    // the same additions in every warp, with the operands of some exchanged: the same sum everywhere
+    const float tot = warp_sum((tid & 31) < (int)(blockDim.x >> 5) ? part[turn][tid & 31] : 0.f);
     const float rs = 1.f / sqrtf(tot / (float)H + a.eps);
 
     T* y = a.y ? static_cast<T*>(a.y) + row * a.y_stride : nullptr;
