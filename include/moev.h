@@ -420,6 +420,10 @@ moev_status moev_cache_append(const moev_kv_cache* cache, const moev_draft_batch
  * A draft sees the context and, of the drafts, itself and its ancestors; with window > 0 of all these
  * only the last window positions.  scores are multiplied by scale (> 0); sinks [n_heads] float32 (or
  * NULL) join the denominator.  lse [n_tokens, n_heads] float32 (or NULL): natural log of the denominator.
+ * Roundings: q is held to 2^-12 of an element or 2^-18 of its row's largest, whichever is more; scores, sums and lse are
+ * binary32; a key's probability times its page's V scale is rounded once to 11 bits (2^-11), or by 2^-28 of the row's largest
+ * such product of a key whose V is not all zero, whichever is more (V scales below 2^-48 of the sequence's largest: or
+ * by 2^-76 of the largest probability times that scale).  Pages that a row does not see or gives no weight do not enter.
  * workspace: moev_cache_attend_workspace bytes for the same sizes (16-byte aligned; 0 = none needed);
  * its contents do not matter before a call or after it, but calls that may overlap need one each. */
 size_t moev_cache_attend_workspace(const moev_kv_cache* cache, const moev_draft_batch* batch, int32_t n_heads, int32_t window);

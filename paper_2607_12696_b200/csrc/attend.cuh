@@ -14,14 +14,16 @@
 // element or 2^-12 of the element, whichever is more.  Up to R = 64 the terms stand side by side as 3 R columns, added as
 // they are read: an instruction takes about 75 cycles however narrow it is; at R = 128 they add in one accumulator.
 // The second product runs in kind::f16: V codes, exact in f16, are widened on their way into tensor memory, which
-// holds the A operand (16 KB of codes per tile, whatever R), and p is rounded once to f16 (2^-11).  In 8 bits p would need
-// two terms and leave the reference below 3 bits of room.
-// The scale of a page's K multiplies its scores, that of its V the probabilities relative to the largest V scale of late.
+// holds the A operand (16 KB of codes per tile, whatever R).  In 8 bits p would need two terms and leave the reference below
+// 3 bits of room.  The scale of a page's K multiplies its scores, that of its V the probabilities, in binary32, and their
+// product is rounded once to f16 (2^-11; 2^-25 in units in which a row's largest is 2^3 or more).
 //
 // In S^T a thread is a key (one page, one scale) and its registers are rows, so a maximum over keys would go across
-// lanes.  It is not taken: the reference m_r only has to be near it.  p = 2^(s - m_r) may reach 2^12 in f16; only
-// when some score exceeds that (in the first tile, then hardly ever) the rows' four warps take the maxima, move m_r and
-// rescale O and the denominators.  Those are per thread, summed across lanes once at the end.
+// lanes.  It is not taken: the reference m_r of p = 2^(s - m_r) only has to keep p * (V scale) near the top of f16, so it
+// follows the largest s + log2(V scale) among the keys that the row sees and whose V is not all zero: a page with a large scale
+// that a row does not see, gives no weight or that holds zeros takes no digits from the others.  Only when a product would
+// exceed 2^15.9 (in the first tile, then hardly ever) the rows' four warps take the maxima, move m_r and rescale O and the
+// denominators.  Those are binary32, of p itself, per thread, summed across lanes once at the end.
 //
 // Roles: one warp loads (TMA), one thread issues the MMAs, groups of four warps do the softmax of a share of the rows each
 // (tensor memory gives a warp a quarter of the lanes) and widen V.  S is double-buffered: S of tile i + 1 is computed
@@ -35,9 +37,9 @@
 //
 // Bound, as measured on B200 (us; bytes at 6.5 TB/s and operations at 1.67 PFLOP/s allow the time in brackets): one draft, 16
 // rows, 4096 keys 13 (0.7): two launches, set-up, one tile and the join, each a chain of trips to memory; 64 drafts x 16
-// heads over 16 000 keys 124 (20): the softmax warps' instructions, 5 800 cycles a tile of 128 x 128, of which the tensor
+// heads over 16 000 keys 130 (20): the softmax warps' instructions, 5 800 cycles a tile of 128 x 128, of which the tensor
 // core needs 1 800; 32 ragged sequences up to 24 000 keys, 32 rows 205 (121): 3 500 cycles a tile of 32 KB on either of an
-// SM's two CTAs, two thirds of the issue slots, 3.9 TB/s; window of 128, 64 rows, 16 sequences 16 (0.5): three masked
+// SM's two CTAs, two thirds of the issue slots, 3.9 TB/s; window of 128, 64 rows, 16 sequences 17 (0.5): three masked
 // tiles a CTA.  The same work on mma.sync with the rows as the wide operand took 187 and 333 us for the second and third.
 #pragma once
 #include <cuda.h>
@@ -53,8 +55,10 @@ using kv::Drafts;
 using kv::Seq;
 
 constexpr int kKeys = 128;                 // keys of a tile
-// p = 2^(s - m_r) may reach 2^12 and a V scale 8 times the accumulators' unit: 2^15 in f16
-constexpr float kLimit = 12.f, kUnitUp = 8.f, kUnitDown = 1.f / 64.f;
+// Powers of two: what p * (V scale) may reach in f16, and what its largest is brought to when the references move.  V scales are
+// relative to a unit, the largest of the first tile, so that p stays in binary32's range: a scale beyond kUnitUp times
+// that becomes the new unit, one below 2^kSlight counts as that for the references, and so does a key without values.
+constexpr float kLimit = 15.9f, kTop = 3.f, kSlight = -48.f, kUnitUp = 0x1p64f;
 constexpr float kUnseen = -3.0e38f;        // reference of a row that has not seen a key yet
 constexpr unsigned long long kBudgetNs = kDeviceWaitBudgetNs;  // per wait; test builds can make the last V tile stay out
 
@@ -76,6 +80,17 @@ struct Args {
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float log2_fast(float x) {  // -inf for 0
+  float r;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// Two values as f16, at most the largest finite one (a key whose V is zero may be beyond that).
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
 // Reduces N values (a power of two up to 32) over the warp's lanes: every exchange halves the values a lane holds, N - 1
@@ -251,8 +266,12 @@ struct Ctl {
   uint64_t k_full[3], k_empty[3], v_full[3], v_empty[3];
   uint64_t s_full[2], s_empty[2], p_full, o_full, q_full, drain;
   alignas(16) float rcm[R / 2][4];  // per two rows: factors from raw scores to powers of two | minus the references m
-  float fac_l[R], fac_o[R];
+  float fac_l[R], fac_o[R];     // what moving a reference multiplies; in the end fac_l: the row's accumulators
+  float peak[R];                // largest reference so far
   float wmax[4][R], lsum[4][R];
+  // by quarter of the dimensions and 32 words per group: byte k of word w is not zero where some V code of key 4 w + k is not.
+  // With 128 rows a group's words take the place of its own lsum, which is written after the last tile
+  uint32_t valued[R == 128 ? 1 : 4 * 128];
   alignas(16) float ks[3][8], vs[3][8];  // by V stage: scales of a tile's 16-key pieces
   alignas(16) int pid[3][8];             // and their pages
   uint32_t vis[2][R][4];        // by tile parity: draft of the tile sees key (bits)
@@ -263,7 +282,6 @@ struct Ctl {
   int at_units, at_segs;        // before the sequence in which this CTA's run begins ...
   int at_seq;                   // ... and that sequence
   Seq at;
-  float fin[R];                 // what a row's accumulators are multiplied by in the end
   float vmax[3];                // by V stage: largest V scale of the tile ...
   int all_there[3];             // ... and whether each of its keys has a page
   int any_nan;                  // some entry of nan_row is not zero
@@ -604,6 +622,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         if ((z % kPer) == 0) {
           S.rcm[r / 2][r & 1] = a.scale_log2 * back;
           S.rcm[r / 2][2 + (r & 1)] = -kUnseen;
+          S.peak[r] = kUnseen;
           S.row[r] = live ? make_int2(s.lo + i, hq) : make_int2(-1, 0);
         }
         if (ex == 128) {  // infinities become NaN: a row with one has NaN scores, as inf * 0 and inf - inf have it
@@ -637,13 +656,14 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
       float l[RH];
 #pragma unroll
       for (int r = 0; r < RH; ++r) l[r] = 0.f;
-      float unit_of[RH / RC], inv_of[RH / RC];  // V scale that the accumulators of each part of the rows are in units of, its reciprocal
+      float unit_of[RH / RC], inv_of[RH / RC];  // V scale that each part of the rows is in units of, its reciprocal
 #pragma unroll
       for (int c = 0; c < RH / RC; ++c) unit_of[c] = inv_of[c] = 0.f;
       const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
       // this key's row of P; 16-byte piece c of it is at c ^ p_xor
       uint8_t* const p_row0 = smem + C::oP + (r0 / 64) * C::kPBlock + key * C::kPRow;
       const int p_xor = C::kPRow == 128 ? key & 7 : C::kPRow == 64 ? (key >> 1) & 3 : (key >> 2) & 1;
+      uint32_t(*const valued)[128] = reinterpret_cast<uint32_t(*)[128]>(R == 128 ? reinterpret_cast<uint32_t*>(S.lsum) : S.valued);
       uint32_t v_off[8 / G];
 #pragma unroll
       for (int z = 0; z < 8 / G; ++z) v_off[z] = v_piece<D>(quad * 32 + lane, group * (8 / G) + z, page_log2);
@@ -678,7 +698,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         const bool plain = !masked && S.all_there[sv];  // every key is there and every row sees it
         const uint32_t s_at = tmem + lane_base + (ct % SB) * C::kSCols + r0;
         uint8_t* const p_row = p_row0 + (ct % C::kPBufs) * C::kP;
-        bool leave = false;
+        bool leave = false, looked = false, zeros = false;
 #pragma unroll
         for (int rc = 0; rc < RH; rc += RC) {  // RC of this thread's rows at a time
           float v[RC];
@@ -720,9 +740,10 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
           };
           load_scores();
           float& u = unit_of[rc / RC];
-          const bool unit = vm > 0.f && (vm > u * kUnitUp || vm < u * kUnitDown);  // the same in the group's threads
+          const bool unit = vm > u * kUnitUp;  // the same in the group's threads
           bool move = it == 0;  // there is no reference yet
           if (it > 0) {
+            const float lv = fmaxf(log2_fast(v_scale * inv_of[rc / RC]), kSlight);
             float tmax = ok ? -INFINITY : INFINITY;
 #pragma unroll
             for (int r = 0; r < RC; r += 2) {
@@ -730,35 +751,73 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
               fma2(v[r], v[r + 1], q.x, q.y, q.z, q.w);
               tmax = fmaxf(tmax, fmaxf(v[r], v[r + 1]));
             }
-            move = any_of(tmax > kLimit || unit, 3 + group, 128);
+            move = any_of(tmax + lv > kLimit || unit, 3 + group, 128);
           }
           if (move) {
-            if (any_of(!ok, 3 + group, 128)) {  // a warp that gave up stays with the others' barriers until here: all of them leave
-              leave = true;
-              break;
+            const uint8_t* vt = smem + C::oV + sv * C::kTile;
+            bool ask = !ok;
+            if (!looked) {  // a key with a value in one of four dimensions is none of the zero ones
+              uint32_t some = 0;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) some |= vt[v_piece<D>(e * (D / 4) + 1, key >> 4, page_log2) + (key & 15)];
+              ask = ask || (there && k0 + key < k_all && !(some & 0x7fu));
+              looked = true;
             }
-            // move the references to the maxima and the unit to the tile's largest V scale.  From the scores themselves:
-            // relative to the reference of a row that has seen nothing they have lost their digits
+            if (any_of(ask, 3 + group, 128)) {
+              if (any_of(!ok, 3 + group, 128)) {  // a warp that gave up stays with the others' barriers until here: all of them leave
+                leave = true;
+                break;
+              }
+              // which keys have values: a lane has a dimension, the warp's lanes are joined
+              zeros = true;
+              if (quad * 32 < D) {
+                uint32_t mine = 0;
+#pragma unroll 1
+                for (int seg = 0; seg < 8; ++seg) {
+                  const uint4 w = *reinterpret_cast<const uint4*>(vt + v_piece<D>(quad * 32 + lane, seg, page_log2));
+                  const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    const uint32_t any = __reduce_or_sync(0xffffffffu, ww[e] & 0x7f7f7f7fu);
+                    if (lane == 4 * seg + e) mine = any;
+                  }
+                }
+                valued[quad][group * 32 + lane] = mine;
+              }
+              ptx::named_barrier(3 + group, 128);
+            }
+            // move the references to the maxima.  From the scores themselves: relative to the reference of a row that has seen
+            // nothing they have lost their digits
             if (it > 0) load_scores();
+            const float u_new = unit ? vm : u, inv = u_new > 0.f ? 1.f / u_new : 0.f;
+            uint32_t values = zeros ? 0u : 0xffffffffu;
+#pragma unroll 1
+            for (int z = 0; zeros && z < D / 32; ++z) values |= valued[z][group * 32 + (key >> 2)];
+            const float lv = (values >> (8 * (key & 3))) & 0xffu ? fmaxf(log2_fast(v_scale * inv), kSlight) : kSlight;
             float x[RC];
 #pragma unroll
-            for (int r = 0; r < RC; ++r) x[r] = v[r] = v[r] * S.rcm[(r0 + rc + r) / 2][r & 1];
+            for (int r = 0; r < RC; ++r) {
+              v[r] *= S.rcm[(r0 + rc + r) / 2][r & 1];
+              x[r] = v[r] + lv;
+            }
             const float top = warp_reduce<RC, true>(x, lane);
             S.wmax[quad][r0 + rc + reduced_index<RC>(lane)] = top;
             ptx::named_barrier(3 + group, 128);
-            const float u_new = unit ? vm : u;
             if (quad == 0 && lane < RC) {
               const int r = r0 + rc + lane;
-              const float old = -S.rcm[r / 2][2 + (r & 1)];
-              const float m = fmaxf(fmaxf(old, fmaxf(S.wmax[0][r], S.wmax[1][r])), fmaxf(S.wmax[2][r], S.wmax[3][r]));
-              const float fl = exp2_fast(old - m);
+              const float old = -S.rcm[r / 2][2 + (r & 1)], peak = S.peak[r];
+              const float turn = u > 0.f && unit ? log2_fast(u) - log2_fast(u_new) : 0.f;  // what is there, in the new unit
+              // not far below an earlier one: the denominators stay in range however often the unit grows
+              const float least = fmaxf(old + turn, peak + kSlight);
+              const float m = fmaxf(least, fmaxf(fmaxf(S.wmax[0][r], S.wmax[1][r]), fmaxf(S.wmax[2][r], S.wmax[3][r])) - kTop);
               S.rcm[r / 2][2 + (r & 1)] = -m;
-              S.fac_l[r] = fl;
-              S.fac_o[r] = fl * (u / u_new);
+              S.peak[r] = fmaxf(peak, m);
+              S.fac_l[r] = exp2_fast(old - m);
+              S.fac_o[r] = exp2_fast(old + turn - m);
             }
             ptx::named_barrier(3 + group, 128);
             u = u_new;
-            inv_of[rc / RC] = u > 0.f ? 1.f / u : 0.f;
+            inv_of[rc / RC] = inv;
 #pragma unroll
             for (int r = 0; r < RC; ++r) {
               l[rc + r] *= S.fac_l[r0 + rc + r];
@@ -784,14 +843,14 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&S.s_empty[ct % SB]);
           }
-          const __half2 f = __float2half2_rn(v_scale * inv_of[rc / RC]);
+          const float f = v_scale * inv_of[rc / RC];
           uint32_t p[RC / 2];
 #pragma unroll
           for (int r = 0; r < RC; r += 2) {
-            const float p0 = exp2_fast(v[r]), p1 = exp2_fast(v[r + 1]);
+            float p0 = exp2_fast(v[r]), p1 = exp2_fast(v[r + 1]);
             add2(l[rc + r], l[rc + r + 1], p0, p1);
-            const __half2 h = __hmul2(__floats2half2_rn(p0, p1), f);
-            p[r / 2] = *reinterpret_cast<const uint32_t*>(&h);
+            mul2(p0, p1, f);
+            p[r / 2] = pack_f16(p0, p1);
           }
           // a single P is free once the second product of the tile before has ended
           if (C::kPBufs == 1 && it > 0 && rc == 0) ok = wait_warp(&S.o_full, (ct - 1) & 1, &S.abort, a.d.status, lane) && ok;
@@ -885,7 +944,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
               if (a.lse) a.lse[(long long)ro.x * a.n_heads + ro.y] = den == 0.f ? -INFINITY : (m + log2f(den)) * 0.6931471805599453f;
             }
           }
-          S.fin[r] = fin;
+          S.fac_l[r] = fin;
         }
         ptx::named_barrier(3 + group, 128);
         const int d = quad * 32 + lane;
@@ -901,7 +960,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
             }
             float o[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = __uint_as_float(oh[e]) * S.fin[r0 + c + e];
+            for (int e = 0; e < 8; ++e) o[e] = __uint_as_float(oh[e]) * S.fac_l[r0 + c + e];
             if (nans) {
 #pragma unroll
               for (int e = 0; e < 8; ++e)
