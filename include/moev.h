@@ -418,7 +418,8 @@ moev_status moev_cache_append(const moev_kv_cache* cache, const moev_draft_batch
 /* Attention of the drafts over the cache (their own keys are in it).  q, out bf16 [n_tokens, n_heads *
  * head_dim], n_heads a multiple of n_kv_heads (query head h reads kv head h / (n_heads / n_kv_heads)).
  * A draft sees the context and, of the drafts, itself and its ancestors; with window > 0 of all these
- * only the last window positions.  scores are multiplied by scale (> 0); sinks [n_heads] float32 (or
+ * only the last window positions (pages that end before ctx_len + 1 - window may have been given back: their entries in the
+ * page table are not looked at).  scores are multiplied by scale (> 0); sinks [n_heads] float32 (or
  * NULL) join the denominator.  lse [n_tokens, n_heads] float32 (or NULL): natural log of the denominator.
  * Roundings: q is held to 2^-12 of an element or 2^-18 of its row's largest, whichever is more; scores, sums and lse are
  * binary32; a key's probability times its page's V scale is rounded once to 11 bits (2^-11), or by 2^-28 of the row's largest

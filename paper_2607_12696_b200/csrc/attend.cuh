@@ -457,9 +457,10 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         ptx::prefetch_tmap(&tm_v);
       }
       const int pages = kKeys >> page_log2, seg = lane & 7;
+      const int seen_from = a.window > 0 ? s.ctx + 1 - a.window : 0;  // a page that ends before that may be gone: it is not looked up
       auto page_at = [&](int it) {
         const int key = k_begin + it * kKeys + 16 * seg;
-        return it < n_tiles && key < k_all ? kv::page_of(a.d, a.c, b, key >> page_log2) : -1;
+        return it < n_tiles && key < k_all && (key | (page - 1)) >= seen_from ? kv::page_of(a.d, a.c, b, key >> page_log2) : -1;
       };
       // page ids two tiles ahead, scales one: each is a trip to memory that the copies do not wait for
       auto scale_at = [&](int p, float& k, float& v) {
