@@ -395,9 +395,9 @@ typedef struct {
  * a chain, draft i continues draft i - 1.  A sequence may have no draft or no context.
  *   max_drafts >= every sequence's drafts (<= 1024 with parents), max_len >= every ctx_len + drafts:
  * host bounds that size the launches.  The arrays are device data: a sequence that breaks the bounds is
- * left out, a page id outside the pool hides its keys, and both set *status (may be NULL; 1 sequence,
+ * left out, a page id outside the pool hides its keys, and both raise *status (may be NULL; 1 sequence,
  * 2 page id, 3 position behind the rotation table, 4 a bounded wait of the attention kernel ran out and its
- * outputs are undefined; never cleared).  Rows that belong to no sequence are left as they are. */
+ * outputs are undefined; the largest of what is found and what was there, never cleared).  Rows that belong to no sequence are left as they are. */
 typedef struct {
   int32_t n_seq, n_tokens, max_drafts, max_len, table_cols;
   const int32_t *cu, *ctx_len, *page_table, *parent;

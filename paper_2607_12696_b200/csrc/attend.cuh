@@ -303,7 +303,7 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile in
       if (*abort_flag) return false;
       if (ptx::globaltimer_ns() - t0 > kBudgetNs) {
         *abort_flag = 1;
-        if (status) atomicExch(status, 4);
+        kv::report(status, 4);
         return false;
       }
     }

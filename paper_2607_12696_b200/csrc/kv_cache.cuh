@@ -27,6 +27,11 @@ struct Cache {
   float *ks, *vs;
 };
 
+// The largest code of all that is reported stays: a time-out (4) is not hidden by a sequence or page that was left out.
+__device__ __forceinline__ void report(int32_t* status, int code) {
+  if (status) atomicMax(status, code);
+}
+
 struct Seq {
   int lo, n, ctx;  // first token row, drafts, tokens in the cache before them
 };
@@ -41,7 +46,7 @@ __device__ __forceinline__ Seq sequence(const Drafts& d, int b, int page) {
   const bool ok = s.lo >= 0 && s.n >= 0 && s.n <= d.max_drafts && s.lo <= d.n_tokens - s.n && s.ctx >= 0 &&
                   s.ctx <= d.max_len - s.n && (long long)s.ctx + s.n <= (long long)d.table_cols * page;
   if (!ok) {
-    if (d.status) *d.status = 1;
+    report(d.status, 1);
     s.n = 0;
   }
   return s;
@@ -49,7 +54,7 @@ __device__ __forceinline__ Seq sequence(const Drafts& d, int b, int page) {
 __device__ __forceinline__ int page_of(const Drafts& d, const Cache& c, int b, int col) {
   const int p = d.table[(long long)b * d.table_cols + col];
   if (p >= 0 && p < c.n_pages) return p;
-  if (d.status) *d.status = 2;
+  report(d.status, 2);
   return -1;
 }
 // Parent of draft i, -1 for one that hangs on the context; anything but an earlier draft of the sequence counts as that.
@@ -168,7 +173,7 @@ __global__ void __launch_bounds__(256) cache_append_kernel(const AppendArgs a) {
       }
       int p = s.ctx + depth;
       if (p >= a.rope_rows) {
-        if (a.d.status) *a.d.status = 3;
+        report(a.d.status, 3);
         p = a.rope_rows - 1;
       }
       pos[r] = p;
