@@ -462,7 +462,8 @@ typedef struct {
  * sequence (attention output zero) would widen the expert union.  workspace: moev_verify_blocks_workspace bytes for the
  * same sizes (16-byte aligned, contents of no matter), one per call in flight.  blocks and outs are HOST arrays of
  * n_blocks entries whose pointers are DEVICE pointers.  Everything but the MoE layers' own pointers (moev_verify checks those
- * when it is their turn) is checked before the first launch.  Asynchronous on cuda_stream. */
+ * when it is their turn) is checked before the first launch.  Asynchronous on cuda_stream; a time-out of the attention kernel is
+ * reported by moev_status_sync like one of the MoE layers'. */
 size_t moev_verify_blocks_workspace(const moev_ctx* ctx, int32_t n_blocks, const moev_block* blocks, const moev_draft_batch* batch,
                                     const moev_block_options* options);
 moev_status moev_verify_blocks(moev_ctx* ctx, int32_t n_blocks, const moev_block* blocks, const moev_draft_batch* batch,

@@ -12,6 +12,7 @@
 
 namespace moev {  // moev_api.cu
 const moev_config& ctx_config(const moev_ctx* c);
+int32_t* ctx_status_word(const moev_ctx* c);
 moev_status ctx_fail(moev_ctx* c, moev_status st, const char* text);
 }  // namespace moev
 
@@ -237,6 +238,43 @@ cudaError_t launch_attend_d(const att::Args& a, int rows, cudaStream_t st) {
   return launch(att::attend_combine_kernel<D>, dim3(a.d.max_drafts, (a.n_heads + 3) / 4, a.d.n_seq), dim3(128), 0, st, a, rows);
 }
 
+// moev_cache_attend, also for a context whose status word learns of a time-out
+moev_status attend(const moev_kv_cache* c, const moev_draft_batch* d, const void* q, int64_t q_stride, int32_t n_heads, float scale,
+                   int32_t window, const float* sinks, void* out, int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes,
+                   int32_t* ctx_status, void* cuda_stream) {
+  if (!batch_ok(c, d) || !q || !out || n_heads < 1 || n_heads % c->n_kv_heads || window < 0 || !(scale > 0.f) || scale > kMaxScale) return MOEV_EINVAL;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(sinks, 4) || q_stride % 8 || out_stride % 8) return MOEV_EINVAL;
+  const int64_t row = (int64_t)n_heads * c->head_dim;
+  if (d->n_tokens > 1 && (q_stride < row || out_stride < row)) return MOEV_EINVAL;
+  if (d->n_seq == 0 || d->n_tokens == 0) return MOEV_OK;
+  const Plan p = attend_plan(c, d, n_heads, window);
+  if ((n_heads + 3) / 4 > 65535 || p.units > kMaxUnits) return MOEV_EINVAL;
+  const size_t need = p.table + p.ml + p.o;
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return MOEV_EINVAL;
+  att::Args a{};
+  a.d = drafts_of(d);
+  a.c = cache_of(c);
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.lse = lse;
+  a.sinks = sinks;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  a.table = reinterpret_cast<int2*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(ws + p.table);
+  a.part_o = reinterpret_cast<float*>(ws + p.table + p.ml);
+  a.q_stride = q_stride;
+  a.out_stride = out_stride;
+  a.n_heads = n_heads;
+  a.rep = n_heads / c->n_kv_heads;
+  a.window = window;
+  a.whole = p.whole;
+  a.grid = p.grid;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.ctx_status = ctx_status;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return done(c->head_dim == 64 ? launch_attend_d<64>(a, p.rows, st) : launch_attend_d<128>(a, p.rows, st));
+}
+
 }  // namespace
 
 extern "C" {
@@ -366,36 +404,7 @@ size_t moev_cache_attend_workspace(const moev_kv_cache* c, const moev_draft_batc
 moev_status moev_cache_attend(const moev_kv_cache* c, const moev_draft_batch* d, const void* q, int64_t q_stride, int32_t n_heads, float scale,
                               int32_t window, const float* sinks, void* out, int64_t out_stride, float* lse, void* workspace,
                               size_t workspace_bytes, void* cuda_stream) {
-  if (!batch_ok(c, d) || !q || !out || n_heads < 1 || n_heads % c->n_kv_heads || window < 0 || !(scale > 0.f) || scale > kMaxScale) return MOEV_EINVAL;
-  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(sinks, 4) || q_stride % 8 || out_stride % 8) return MOEV_EINVAL;
-  const int64_t row = (int64_t)n_heads * c->head_dim;
-  if (d->n_tokens > 1 && (q_stride < row || out_stride < row)) return MOEV_EINVAL;
-  if (d->n_seq == 0 || d->n_tokens == 0) return MOEV_OK;
-  const Plan p = attend_plan(c, d, n_heads, window);
-  if ((n_heads + 3) / 4 > 65535 || p.units > kMaxUnits) return MOEV_EINVAL;
-  const size_t need = p.table + p.ml + p.o;
-  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return MOEV_EINVAL;
-  att::Args a{};
-  a.d = drafts_of(d);
-  a.c = cache_of(c);
-  a.q = static_cast<const __nv_bfloat16*>(q);
-  a.out = static_cast<__nv_bfloat16*>(out);
-  a.lse = lse;
-  a.sinks = sinks;
-  uint8_t* ws = static_cast<uint8_t*>(workspace);
-  a.table = reinterpret_cast<int2*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(ws + p.table);
-  a.part_o = reinterpret_cast<float*>(ws + p.table + p.ml);
-  a.q_stride = q_stride;
-  a.out_stride = out_stride;
-  a.n_heads = n_heads;
-  a.rep = n_heads / c->n_kv_heads;
-  a.window = window;
-  a.whole = p.whole;
-  a.grid = p.grid;
-  a.scale_log2 = scale * 1.4426950408889634f;
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  return done(c->head_dim == 64 ? launch_attend_d<64>(a, p.rows, st) : launch_attend_d<128>(a, p.rows, st));
+  return attend(c, d, q, q_stride, n_heads, scale, window, sinks, out, out_stride, lse, workspace, workspace_bytes, nullptr, cuda_stream);
 }
 
 
@@ -493,8 +502,8 @@ moev_status moev_verify_blocks(moev_ctx* ctx, int32_t n_blocks, const moev_block
     STEP(moev_linear_w4(&b.qkv, b.qkv_packed, b.qkv_bias, ws + w.x, H, T, qkv, all, MOEV_ACT_BF16, st), "qkv projection");
     STEP(moev_cache_append(&b.cache, d, qkv + row, all, qkv + row + kv_row, all, o->rope, o->rope_rows, qkv, all, o->n_heads, qkv, all, st), "cache append");
     if (cudaMemsetAsync(ws + w.attn, 0, (size_t)T * row * 2, st) != cudaSuccess) return ctx_fail(ctx, MOEV_ECUDA, "memset failed");
-    STEP(moev_cache_attend(&b.cache, d, qkv, all, o->n_heads, o->scale > 0.f ? o->scale : (float)(1.0 / std::sqrt((double)D)), b.window, b.sinks,
-                           ws + w.attn, row, nullptr, ws + w.attend, w.total - w.attend, st),
+    STEP(attend(&b.cache, d, qkv, all, o->n_heads, o->scale > 0.f ? o->scale : (float)(1.0 / std::sqrt((double)D)), b.window, b.sinks,
+                ws + w.attn, row, nullptr, ws + w.attend, w.total - w.attend, ctx_status_word(ctx), st),
          "attention");
     STEP(moev_linear_w4(&b.o, b.o_packed, b.o_bias, ws + w.attn, row, T, ws + w.o, H, MOEV_ACT_BF16, st), "output projection");
     n.w = b.ffn_norm;

@@ -385,6 +385,7 @@ void launch_simt_ffn_w(moev_ctx* c, const LayerPtrs& L, const void* x, int gamma
 // for the other translation unit of the library (block_api.cu)
 namespace moev {
 __attribute__((visibility("hidden"))) const moev_config& ctx_config(const moev_ctx* c) { return c->cfg; }
+__attribute__((visibility("hidden"))) int32_t* ctx_status_word(const moev_ctx* c) { return c->T.status; }
 __attribute__((visibility("hidden"))) moev_status ctx_fail(moev_ctx* c, moev_status st, const char* text) { return fail(c, st, "%s", text); }
 }  // namespace moev
 

@@ -21,3 +21,10 @@ def result():
 
 def test_a_time_out_stays_in_the_status_word_beside_a_rejected_sequence(result):
     assert result["rejected"] == [[0, 1], [0, 4], [0, 1]]
+
+
+def test_blocks_report_a_time_out_of_their_attention(result):
+    """moev_status_sync says so, with and without a status word of the batch."""
+    quiet, quiet_word, late, late_word = result["blocks"]
+    assert quiet == [0, 0, None] and quiet_word == [0, 0, 0]
+    assert late[0] != 0 and late == [late[0], 0, None] and late_word == [late[0], 0, 4]
