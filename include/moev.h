@@ -405,7 +405,7 @@ typedef struct {
 } moev_draft_batch;
 
 /* Write the drafts' keys and values (bf16 [n_tokens, n_kv_heads * head_dim], row strides multiples of 8
- * elements) to the cache.  rope [rope_rows, head_dim] float32 (head_dim / 2 cosines, then as many sines,
+ * elements, as those of q and q_out) to the cache.  rope [rope_rows, head_dim] float32 (head_dim / 2 cosines, then as many sines,
  * by position), or NULL for no rotation: dimensions i and i + head_dim / 2 of K, and of q where it is
  * given, are rotated in binary32; q_out (may be q) receives the queries in bf16.  A page's scale is the smallest power of
  * two that brings its largest magnitude to 448 or less; a page that held tokens before (ctx_len inside it) keeps
@@ -416,7 +416,7 @@ moev_status moev_cache_append(const moev_kv_cache* cache, const moev_draft_batch
                               int64_t q_stride, int32_t n_heads, void* q_out, int64_t q_out_stride, void* cuda_stream);
 
 /* Attention of the drafts over the cache (their own keys are in it).  q, out bf16 [n_tokens, n_heads *
- * head_dim], n_heads a multiple of n_kv_heads (query head h reads kv head h / (n_heads / n_kv_heads)).
+ * head_dim] (row strides multiples of 8 elements), n_heads a multiple of n_kv_heads (query head h reads kv head h / (n_heads / n_kv_heads)).
  * A draft sees the context and, of the drafts, itself and its ancestors; with window > 0 of all these
  * only the last window positions (pages that end before ctx_len + 1 - window may have been given back: their entries in the
  * page table are not looked at).  scores are multiplied by scale (> 0); sinks [n_heads] float32 (or

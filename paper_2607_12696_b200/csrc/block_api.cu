@@ -158,6 +158,8 @@ bool batch_ok(const moev_kv_cache* c, const moev_draft_batch* d) {
   if (d->parent && d->max_drafts > kv::kMaxTree) return false;
   return d->cu && d->ctx_len && d->page_table;
 }
+// Row stride of a 16-bit tensor of n rows that are read by 16 bytes: of one row it is not looked at.
+bool stride_ok(int64_t stride, int64_t width, int n) { return n <= 1 || (stride >= width && stride % 8 == 0); }
 kv::Drafts drafts_of(const moev_draft_batch* d) {
   return kv::Drafts{d->n_seq, d->n_tokens, d->max_drafts, d->max_len, d->table_cols, d->cu, d->ctx_len, d->page_table, d->parent, d->status};
 }
@@ -243,9 +245,9 @@ moev_status attend(const moev_kv_cache* c, const moev_draft_batch* d, const void
                    int32_t window, const float* sinks, void* out, int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes,
                    int32_t* ctx_status, void* cuda_stream) {
   if (!batch_ok(c, d) || !q || !out || n_heads < 1 || n_heads % c->n_kv_heads || window < 0 || !(scale > 0.f) || scale > kMaxScale) return MOEV_EINVAL;
-  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(sinks, 4) || q_stride % 8 || out_stride % 8) return MOEV_EINVAL;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(sinks, 4)) return MOEV_EINVAL;
   const int64_t row = (int64_t)n_heads * c->head_dim;
-  if (d->n_tokens > 1 && (q_stride < row || out_stride < row)) return MOEV_EINVAL;
+  if (!stride_ok(q_stride, row, d->n_tokens) || !stride_ok(out_stride, row, d->n_tokens)) return MOEV_EINVAL;
   if (d->n_seq == 0 || d->n_tokens == 0) return MOEV_OK;
   const Plan p = attend_plan(c, d, n_heads, window);
   if ((n_heads + 3) / 4 > 65535 || p.units > kMaxUnits) return MOEV_EINVAL;
@@ -362,15 +364,15 @@ moev_status moev_linear_w4(const moev_linear* p, const void* packed, const float
 moev_status moev_cache_append(const moev_kv_cache* c, const moev_draft_batch* d, const void* k, int64_t k_stride, const void* v,
                               int64_t v_stride, const float* rope, int32_t rope_rows, const void* q, int64_t q_stride, int32_t n_heads,
                               void* q_out, int64_t q_out_stride, void* cuda_stream) {
-  if (!batch_ok(c, d) || !k || !v || !aligned(k, 16) || !aligned(v, 16) || k_stride % 8 || v_stride % 8) return MOEV_EINVAL;
+  if (!batch_ok(c, d) || !k || !v || !aligned(k, 16) || !aligned(v, 16)) return MOEV_EINVAL;
   const int64_t kv_row = (int64_t)c->n_kv_heads * c->head_dim;
-  if (d->n_tokens > 1 && (k_stride < kv_row || v_stride < kv_row)) return MOEV_EINVAL;
+  if (!stride_ok(k_stride, kv_row, d->n_tokens) || !stride_ok(v_stride, kv_row, d->n_tokens)) return MOEV_EINVAL;
   if (rope && (rope_rows < 1 || !aligned(rope, 16))) return MOEV_EINVAL;
   if ((q != nullptr) != (q_out != nullptr)) return MOEV_EINVAL;
   if (q) {
     const int64_t q_row = (int64_t)n_heads * c->head_dim;
-    if (n_heads < 1 || n_heads % c->n_kv_heads || !aligned(q, 16) || !aligned(q_out, 16) || q_stride % 8 || q_out_stride % 8) return MOEV_EINVAL;
-    if (d->n_tokens > 1 && (q_stride < q_row || q_out_stride < q_row)) return MOEV_EINVAL;
+    if (n_heads < 1 || n_heads % c->n_kv_heads || !aligned(q, 16) || !aligned(q_out, 16)) return MOEV_EINVAL;
+    if (!stride_ok(q_stride, q_row, d->n_tokens) || !stride_ok(q_out_stride, q_row, d->n_tokens)) return MOEV_EINVAL;
   }
   if (d->n_seq == 0 || d->n_tokens == 0) return MOEV_OK;
   kv::AppendArgs a{};
