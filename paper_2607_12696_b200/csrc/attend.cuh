@@ -295,7 +295,7 @@ size_t smem_bytes(int words, bool tree) {  // + ancestor words of the tile's dra
   return 1024 + Cfg<D, R>::oCtl + sizeof(Ctl<R>) + (tree ? (size_t)R * words * 4 + (size_t)words * 128 : 0);
 }
 
-__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, const Args& a) {
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
   if (ptx::mbar_try_wait(bar, parity)) return true;
   const uint64_t t0 = ptx::globaltimer_ns();
   for (uint32_t it = 1;; ++it) {
@@ -304,8 +304,7 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile in
       if (*abort_flag) return false;
       if (ptx::globaltimer_ns() - t0 > kBudgetNs) {
         *abort_flag = 1;
-        kv::report(a.d.status, 4);
-        if (a.ctx_status) atomicExch(a.ctx_status, kStatusTimeout);
+        kv::report(status, 4);
         return false;
       }
     }
@@ -313,9 +312,9 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile in
 }
 
 // The same for a whole warp: one lane looks.
-__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, const Args& a, int lane) {
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int32_t* status, int lane) {
   int r = 1;
-  if (lane == 0) r = wait(bar, parity, abort_flag, a);
+  if (lane == 0) r = wait(bar, parity, abort_flag, status);
   return __shfl_sync(0xffffffffu, r, 0) != 0;
 }
 
@@ -481,7 +480,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         const int mine = __shfl_sync(0xffffffffu, pid, ((lane & 7) << page_log2) >> 4 & 7);  // page `lane` of the tile
         const bool on = lane < pages && mine >= 0;
         const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, on)) * page * D;
-        if (ct >= KS && !wait_warp(&S.k_empty[sk], ((ct / KS) & 1) ^ 1, &S.abort, a, lane)) break;
+        if (ct >= KS && !wait_warp(&S.k_empty[sk], ((ct / KS) & 1) ^ 1, &S.abort, a.d.status, lane)) break;
         uint8_t* dst = smem + C::oK + sk * C::kTile + (lane & 7) * page * D;
         if (lane == 0) {
           ptx::mbar_arrive_expect_tx(&S.k_full[sk], bytes);
@@ -490,7 +489,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         __syncwarp();
         if (on) ptx::tma_load_2d(dst, &tm_k, &S.k_full[sk], 0, (mine * a.c.heads + head) << page_log2, ptx::kPolicyEvictNormal);
         if (MOEV_TEST_WITHHOLD() && it == n_tiles - 1) break;
-        if (ct >= VS && !wait_warp(&S.v_empty[sv], ((ct / VS) & 1) ^ 1, &S.abort, a, lane)) break;
+        if (ct >= VS && !wait_warp(&S.v_empty[sv], ((ct / VS) & 1) ^ 1, &S.abort, a.d.status, lane)) break;
         if (lane < 8) {
           S.ks[sv][lane] = ks;
           S.vs[sv][lane] = vs;
@@ -531,8 +530,8 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         bool ok = true;
         auto scores = [&](int it) {
           const int ct = gt + it, st = ct % KS, u = ct % SB;
-          ok = ok && wait(&S.k_full[st], (ct / KS) & 1, &S.abort, a);
-          if (ct >= SB) ok = ok && wait(&S.s_empty[u], ((ct / SB) & 1) ^ 1, &S.abort, a);
+          ok = ok && wait(&S.k_full[st], (ct / KS) & 1, &S.abort, a.d.status);
+          if (ct >= SB) ok = ok && wait(&S.s_empty[u], ((ct / SB) & 1) ^ 1, &S.abort, a.d.status);
           if (!ok) return;
           ptx::tc_fence_after();
           const uint32_t ka = kb + st * (C::kTile / 16);
@@ -545,12 +544,12 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
           ptx::mma_commit(&S.s_full[u]);
         };
         {
-          ok = wait(&S.q_full, piece & 1, &S.abort, a);
+          ok = wait(&S.q_full, piece & 1, &S.abort, a.d.status);
           if (n_tiles > 0) scores(0);
         }
         for (int it = 0; it < n_tiles && ok; ++it) {
           if (it + 1 < n_tiles) scores(it + 1);
-          ok = ok && wait(&S.p_full, (gt + it) & 1, &S.abort, a);
+          ok = ok && wait(&S.p_full, (gt + it) & 1, &S.abort, a.d.status);
           if (!ok) break;
           ptx::tc_fence_after();
 #pragma unroll
@@ -692,8 +691,8 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
           }
           ptx::named_barrier(3 + group, 128);
         }
-        ok = wait_warp(&S.v_full[sv], (ct / VS) & 1, &S.abort, a, lane) && ok;
-        ok = wait_warp(&S.s_full[ct % SB], (ct / SB) & 1, &S.abort, a, lane) && ok;
+        ok = wait_warp(&S.v_full[sv], (ct / VS) & 1, &S.abort, a.d.status, lane) && ok;
+        ok = wait_warp(&S.s_full[ct % SB], (ct / SB) & 1, &S.abort, a.d.status, lane) && ok;
         ptx::tc_fence_after();
         const float k_scale = S.ks[sv][key >> 4], v_scale = S.vs[sv][key >> 4];
         const bool there = S.pid[sv][key >> 4] >= 0;
@@ -827,7 +826,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
               v[r] += S.rcm[(r0 + rc + r) / 2][2 + (r & 1)];
             }
             if (it > 0) {
-              ok = wait_warp(&S.o_full, (ct - 1) & 1, &S.abort, a, lane) && ok;  // the second product of tile it - 1 has ended
+              ok = wait_warp(&S.o_full, (ct - 1) & 1, &S.abort, a.d.status, lane) && ok;  // the second product of tile it - 1 has ended
               ptx::tc_fence_after();
               uint32_t o[RC];
               const uint32_t at = tmem + lane_base + C::kO + r0 + rc;
@@ -856,7 +855,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
             p[r / 2] = pack_f16(p0, p1);
           }
           // a single P is free once the second product of the tile before has ended
-          if (C::kPBufs == 1 && it > 0 && rc == 0) ok = wait_warp(&S.o_full, (ct - 1) & 1, &S.abort, a, lane) && ok;
+          if (C::kPBufs == 1 && it > 0 && rc == 0) ok = wait_warp(&S.o_full, (ct - 1) & 1, &S.abort, a.d.status, lane) && ok;
 #pragma unroll
           for (int c = 0; c < RC / 8; ++c)
             *reinterpret_cast<uint4*>(p_row + ((((r0 + rc) % 64) / 8 + c) ^ p_xor) * 16) = make_uint4(p[4 * c], p[4 * c + 1], p[4 * c + 2], p[4 * c + 3]);
@@ -865,7 +864,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
           ok = false;
           break;
         }
-        if (C::kPBufs == 2 && it > 0) ok = wait_warp(&S.o_full, (ct - 1) & 1, &S.abort, a, lane) && ok;  // the widened V is free
+        if (C::kPBufs == 2 && it > 0) ok = wait_warp(&S.o_full, (ct - 1) & 1, &S.abort, a.d.status, lane) && ok;  // the widened V is free
         // V: this thread's dimension (its lane of tensor memory), its group's share of the keys
         const int d = quad * 32 + lane;
         if (quad * 32 < D) {
@@ -923,7 +922,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
         }
       }
       // ---- results
-      if (ok && n_tiles > 0) ok = wait_warp(&S.o_full, (gt + n_tiles - 1) & 1, &S.abort, a, lane);
+      if (ok && n_tiles > 0) ok = wait_warp(&S.o_full, (gt + n_tiles - 1) & 1, &S.abort, a.d.status, lane);
       ptx::tc_fence_after();
       const float sum = warp_reduce<RH, false>(l, lane);
       S.lsum[quad][r0 + reduced_index<RH>(lane)] = sum;
@@ -1001,6 +1000,7 @@ __global__ void __launch_bounds__(Cfg<D, R>::kThreads, Cfg<D, R>::kCtas) attend_
     }
   }
   if (S.abort && warp == 4 * G && lane == 0) {  // copies in flight land before the shared memory is given back
+    if (a.ctx_status) atomicExch(a.ctx_status, kStatusTimeout);
     ptx::drain_ring(S.k_full, KS, S.k_it, kBudgetNs);
     ptx::drain_ring(S.v_full, VS, S.v_it, kBudgetNs);
   }
