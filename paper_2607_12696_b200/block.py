@@ -217,8 +217,10 @@ def verify_blocks(verifier, blocks: list, batch: DraftBatch, hidden: torch.Tenso
     if final_norm is not None and (final_norm.dtype != torch.bfloat16 or final_norm.shape != (H,) or not final_norm.is_contiguous()
                                    or final_out.dtype != torch.bfloat16 or final_out.shape != (T, H) or not final_out.is_contiguous()):
         _bad(f"final_norm, final_out: expected contiguous bfloat16 [{H}] and [{T}, {H}]")
-    _same_device(hidden, batch.cu, rope, final_norm, final_out, workspace, *[o[f] for o in outs for f in ("y", "n_active")],
+    _same_device(hidden, batch.cu, rope, final_norm, final_out, workspace, *[o.get(f) for o in outs for f in _OUT_FIELDS],
                  *[t for b in blocks for t in (b.cache.k, b.attn_norm, b.ffn_norm, b.sinks, b.qkv.packed, b.o.packed)])
+    if not hidden.is_cuda or hidden.get_device() != torch.cuda.current_device():
+        _bad(f"tensors must be on the current CUDA device, got {hidden.device}")
     for o in outs:
         if o["y"].dtype != torch.bfloat16 or o["y"].shape[0] < T or o["y"].shape[1:] != (H,) or not o["y"].is_contiguous():
             _bad(f"outs: y must be contiguous bfloat16 [{T}, {H}]")
