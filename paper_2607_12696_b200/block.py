@@ -33,6 +33,12 @@ def _bad(text: str):
     raise MoevError(_EINVAL, text)
 
 
+def _int32(**named):
+    for name, v in named.items():
+        if not -2 ** 31 <= v < 2 ** 31:
+            _bad(f"{name}: {v} does not fit in 32 bits")
+
+
 def _same_device(first: torch.Tensor, *others):
     for t in others:
         if t is not None and t.device != first.device:
@@ -57,6 +63,7 @@ class W4Linear:
             _bad(f"codes: expected contiguous uint8 [N, K / 2], got {tuple(codes.shape)} {codes.dtype}")
         N, K = codes.shape[0], codes.shape[1] * 2
         self.N, self.K, self.wfmt, self.group = N, K, wfmt, group
+        _int32(N=N, K=K, wfmt=wfmt, group=group)
         self._c = _Linear(N, K, wfmt, group)
         size = lib().moev_w4_packed_bytes(C.byref(self._c))
         if size == 0:
@@ -94,6 +101,7 @@ class KvCache:
             if t.dtype not in (torch.uint8, torch.float8_e4m3fn) or not t.is_contiguous():
                 _bad(f"{name}: expected contiguous uint8 or float8_e4m3fn, got {t.dtype}")
         n, heads, page, D = k.shape
+        _int32(pages=n, heads=heads)
         for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
             if t.dtype != torch.float32 or t.shape != (n, heads) or not t.is_contiguous():
                 _bad(f"{name}: expected contiguous float32 [{n}, {heads}]")
@@ -129,6 +137,7 @@ class DraftBatch:
         _same_device(cu, ctx_len, page_table, parent, status)
         self.cu, self.ctx_len, self.page_table, self.parent, self.status = cu, ctx_len, page_table, parent, status
         self.max_drafts, self.max_len = max_drafts, max_len
+        _int32(sequences=n, max_drafts=max_drafts, max_len=max_len, columns=page_table.shape[1])
         self._c = _DraftBatch(n, 0, max_drafts, max_len, page_table.shape[1], cu.data_ptr(), ctx_len.data_ptr(), page_table.data_ptr(),
                               None if parent is None else parent.data_ptr(), None if status is None else status.data_ptr())
         self._at = C.addressof(self._c)
@@ -152,6 +161,7 @@ def cache_append(cache: KvCache, batch: DraftBatch, k: torch.Tensor, v: torch.Te
 
 def cache_attend_workspace(cache: KvCache, batch: DraftBatch, n_heads: int, window: int = 0) -> torch.Tensor:
     """A workspace for cache_attend calls with these bounds (it does not depend on the number of token rows)."""
+    _int32(n_heads=n_heads, window=window)
     size = lib().moev_cache_attend_workspace(C.byref(cache._c), C.byref(batch._c), n_heads, window)
     return torch.empty(size, dtype=torch.uint8, device=cache.k.device)
 
@@ -189,6 +199,7 @@ class Block:
                 _bad(f"{name}: expected {H} contiguous bfloat16 values")
         if self.sinks is not None and (self.sinks.dtype != torch.float32 or self.sinks.shape != (n_heads,) or not self.sinks.is_contiguous()):
             _bad(f"sinks: expected contiguous float32 [{n_heads}]")
+        _int32(window=self.window)
         return _Block(self.attn_norm.data_ptr(), self.ffn_norm.data_ptr(), self.qkv._c, self.o._c, self.qkv._args[1], self.o._args[1],
                       self.qkv._args[2], self.o._args[2], _ptr(self.sinks), self.window, self.cache._c, self.layer)
 
@@ -203,6 +214,7 @@ def verify_blocks(verifier, blocks: list, batch: DraftBatch, hidden: torch.Tenso
     if hidden.dtype != torch.bfloat16 or hidden.dim() != 2 or hidden.shape[1] != H or not hidden.is_contiguous():
         _bad(f"hidden: expected contiguous bfloat16 [n_tokens, {H}], got {tuple(hidden.shape)} {hidden.dtype}")
     T, n = hidden.shape[0], len(blocks)
+    _int32(token_rows=T, n_heads=n_heads, positions=0 if rope is None else rope.shape[0])
     if len(outs) != n or not n:
         _bad(f"{n} blocks and {len(outs)} outputs")
     if batch.parent is not None and batch._parents < T:
