@@ -1,6 +1,7 @@
 // Host side of the operators around the MoE layer (the second part of include/moev.h): argument
 // checks, launch rules, launches.  Stateless: no context, nothing allocated, nothing kept.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 
@@ -27,11 +28,15 @@ constexpr long long kMaxUnits = 0x3fffffff;  // tiles of an attention call
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 int sm_count() {
-  static int n[64] = {};  // by device; a constant of the hardware
+  static std::atomic<int> known[64];  // by device; a constant of the hardware, whichever thread finds it
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-  if (n[dev] == 0 && cudaDeviceGetAttribute(&n[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
-  return n[dev];
+  int n = known[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
+    known[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
 }
 
 // Dependent launch: the kernel may become resident while its predecessor drains; it waits (griddepcontrol.wait) before
