@@ -337,7 +337,7 @@ size_t moev_route_topk_static_scratch_floats(int32_t H, int32_t E, int32_t gamma
  * context; the paper takes these from its host framework.  The operators below are stateless like
  * moev_select_drafts: no context, nothing allocated, nothing kept between calls, everything
  * enqueued on cuda_stream of the current device, MOEV_EINVAL before anything is launched.  Row strides are in
- * elements and are not looked at where a tensor has one row.
+ * elements and are not looked at where a tensor has one row; tensors of no rows, and a batch's arrays without sequences, may be NULL.
  * ====================================================================================== */
 
 /* s = x + residual (binary32),  y = s / sqrt(mean(s^2) + eps) * w, and optionally the FP8 1x128

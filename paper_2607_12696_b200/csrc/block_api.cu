@@ -161,7 +161,7 @@ bool batch_ok(const moev_kv_cache* c, const moev_draft_batch* d) {
   // coordinates of the rows of K and V are 32 bits wide
   if ((long long)c->n_pages * c->n_kv_heads * std::max(c->page, c->head_dim) > 0x7fffffffLL) return false;
   if (d->parent && d->max_drafts > kv::kMaxTree) return false;
-  return d->cu && d->ctx_len && d->page_table;
+  return d->n_seq == 0 || (d->cu && d->ctx_len && d->page_table);
 }
 // Row stride of a 16-bit tensor of n rows that are read by 16 bytes: of one row it is not looked at.
 bool stride_ok(int64_t stride, int64_t width, int n) { return n <= 1 || (stride >= width && stride % 8 == 0); }
@@ -249,7 +249,7 @@ cudaError_t launch_attend_d(const att::Args& a, int rows, cudaStream_t st) {
 moev_status attend(const moev_kv_cache* c, const moev_draft_batch* d, const void* q, int64_t q_stride, int32_t n_heads, float scale,
                    int32_t window, const float* sinks, void* out, int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes,
                    int32_t* ctx_status, void* cuda_stream) {
-  if (!batch_ok(c, d) || !q || !out || n_heads < 1 || n_heads % c->n_kv_heads || window < 0 || !(scale > 0.f) || scale > kMaxScale) return MOEV_EINVAL;
+  if (!batch_ok(c, d) || (d->n_tokens > 0 && (!q || !out)) || n_heads < 1 || n_heads % c->n_kv_heads || window < 0 || !(scale > 0.f) || scale > kMaxScale) return MOEV_EINVAL;
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(sinks, 4)) return MOEV_EINVAL;
   const int64_t row = (int64_t)n_heads * c->head_dim;
   if (!stride_ok(q_stride, row, d->n_tokens) || !stride_ok(out_stride, row, d->n_tokens)) return MOEV_EINVAL;
@@ -289,8 +289,9 @@ extern "C" {
 moev_status moev_add_rmsnorm(const moev_norm* p, void* cuda_stream) {
   if (!p || p->n < 0 || p->H < 1 || p->H > kMaxNorm || p->afmt < 0 || p->afmt > MOEV_ACT_BF16 || p->wfmt < 0 || p->wfmt > MOEV_ACT_BF16)
     return MOEV_EINVAL;
-  if (p->act_quant < 0 || p->act_quant > MOEV_ACTQ_FP8_B128_POW2 || !(p->eps >= 0.f)) return MOEV_EINVAL;
-  if (!p->x || !p->w || (!p->y && !p->codes && !p->residual_out) || (p->act_quant != 0) != (p->codes != nullptr) || (p->codes != nullptr) != (p->scales != nullptr))
+  if (p->act_quant < 0 || p->act_quant > MOEV_ACTQ_FP8_B128_POW2 || !(p->eps >= 0.f) || !p->w) return MOEV_EINVAL;
+  if (p->n == 0) return MOEV_OK;  // tensors of no rows have no address
+  if (!p->x || (!p->y && !p->codes && !p->residual_out) || (p->act_quant != 0) != (p->codes != nullptr) || (p->codes != nullptr) != (p->scales != nullptr))
     return MOEV_EINVAL;
   const int es = p->afmt == MOEV_ACT_BF16 ? 2 : 4, ws = p->wfmt == MOEV_ACT_BF16 ? 2 : 4;
   bool vec = p->H % 8 == 0 && aligned(p->w, 16) && aligned(p->codes, 8) && (!p->codes || p->n == 1 || p->codes_stride % 8 == 0);
@@ -302,7 +303,6 @@ moev_status moev_add_rmsnorm(const moev_norm* p, void* cuda_stream) {
     vec = vec && aligned(ptr[i], 16) && (p->n == 1 || (stride[i] * es) % 16 == 0);
   }
   if (!aligned(p->w, ws) || !aligned(p->scales, 4) || (p->codes && p->n > 1 && p->codes_stride < p->H)) return MOEV_EINVAL;
-  if (p->n == 0) return MOEV_OK;
   NormArgs a{p->x, p->residual, p->w, p->y, p->residual_out, p->codes, p->scales, p->x_stride, p->residual_stride, p->y_stride,
              p->residual_out_stride, p->codes_stride, p->n, p->H, p->act_quant, p->eps};
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -340,7 +340,7 @@ moev_status moev_w4_pack(const moev_linear* p, const void* codes, const void* sc
 
 moev_status moev_linear_w4(const moev_linear* p, const void* packed, const float* bias, const void* x, int64_t x_stride, int32_t n, void* y,
                            int64_t y_stride, int32_t yfmt, void* cuda_stream) {
-  if (!linear_ok(p) || !packed || !x || !y || n < 0 || yfmt < 0 || yfmt > MOEV_ACT_BF16) return MOEV_EINVAL;
+  if (!linear_ok(p) || !packed || (n > 0 && (!x || !y)) || n < 0 || yfmt < 0 || yfmt > MOEV_ACT_BF16) return MOEV_EINVAL;
   if (!aligned(packed, 16) || !aligned(x, 2) || !aligned(y, yfmt == MOEV_ACT_BF16 ? 2 : 4) || !aligned(bias, 4)) return MOEV_EINVAL;
   if (n > 1 && (x_stride < p->K || y_stride < p->N)) return MOEV_EINVAL;
   if (n > 32 * 65535) return MOEV_EINVAL;
@@ -369,7 +369,7 @@ moev_status moev_linear_w4(const moev_linear* p, const void* packed, const float
 moev_status moev_cache_append(const moev_kv_cache* c, const moev_draft_batch* d, const void* k, int64_t k_stride, const void* v,
                               int64_t v_stride, const float* rope, int32_t rope_rows, const void* q, int64_t q_stride, int32_t n_heads,
                               void* q_out, int64_t q_out_stride, void* cuda_stream) {
-  if (!batch_ok(c, d) || !k || !v || !aligned(k, 16) || !aligned(v, 16)) return MOEV_EINVAL;
+  if (!batch_ok(c, d) || (d->n_tokens > 0 && (!k || !v)) || !aligned(k, 16) || !aligned(v, 16)) return MOEV_EINVAL;
   const int64_t kv_row = (int64_t)c->n_kv_heads * c->head_dim;
   if (!stride_ok(k_stride, kv_row, d->n_tokens) || !stride_ok(v_stride, kv_row, d->n_tokens)) return MOEV_EINVAL;
   if (rope && (rope_rows < 1 || !aligned(rope, 16))) return MOEV_EINVAL;

@@ -174,6 +174,13 @@ PyObject* linear_w4(PyObject* const* a) {
   return THPVariable_Wrap(*y);
 }
 
+// Heads of D elements in a row; 0 where a row is not made of those.
+int64_t heads_of(const at::Tensor& q, int64_t D) {
+  int64_t width = 1;
+  for (int64_t i = 1; i < q.dim(); ++i) width *= q.size(i);
+  return q.dim() > 1 && width % D == 0 ? width / D : 0;
+}
+
 moev_draft_batch batch_for(PyObject* o, PyObject* parents, int64_t n_tokens) {
   moev_draft_batch d = *address<moev_draft_batch>(o);
   const long have = integer(parents);
@@ -195,7 +202,7 @@ PyObject* cache_append(PyObject* const* a) {
   int64_t heads = 0, q_stride = 0, o_stride = 0;
   if (q) {
     if (!o) o = q;
-    heads = T ? q->numel() / (T * D) : c->n_kv_heads;
+    heads = heads_of(*q, D);
     q_stride = rows(*q, "q", T, heads * D, at::kBFloat16);
     o_stride = rows(*o, "q_out", T, heads * D, at::kBFloat16);
   } else if (o) {
@@ -217,7 +224,7 @@ PyObject* cache_attend(PyObject* const* a) {
   const int dev = (int)integer(a[3]);
   const at::Tensor& q = tensor(a[4], "q");
   const at::Tensor *out = optional(a[5], "out"), *lse = optional(a[6], "lse"), *sinks = optional(a[9], "sinks"), *ws = optional(a[10], "workspace");
-  const int64_t T = q.dim() ? q.size(0) : 0, D = c->head_dim, heads = T ? q.numel() / (T * D) : c->n_kv_heads;
+  const int64_t T = q.dim() ? q.size(0) : 0, D = c->head_dim, heads = heads_of(q, D);
   const moev_draft_batch d = batch_for(a[1], a[2], T);
   const int64_t q_stride = rows(q, "q", T, heads * D, at::kBFloat16);
   at::Tensor made;
