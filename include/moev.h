@@ -364,7 +364,7 @@ moev_status moev_add_rmsnorm(const moev_norm* p, void* cuda_stream);
 /* y [n, N] = x [n, K] W^T + bias for bf16 rows x and a 4-bit weight W [N, K] with group scales:
  *   MOEV_W_INT4   codes uint8 [N, K / 2], scales bfloat16 [N, K / group], group 32, 64 or 128
  *   MOEV_W_MXFP4  codes uint8 [N, K / 2], scales uint8 [N, K / 32], group 32
- * K is a multiple of 32 and of group; N is free; MXFP4 scales lie between 2^-100 and 2^100.  moev_w4_pack lays a weight out
+ * codes on a 4-byte boundary.  K is a multiple of 32 and of group; N is free; MXFP4 scales lie between 2^-100 and 2^100.  moev_w4_pack lays a weight out
  * once in the order in which the kernel streams it (moev_w4_packed_bytes bytes, 16-byte aligned,
  * caller-owned); moev_linear_w4 reads the packed form.  Products are exact, sums are binary32; y is yfmt (moev_afmt).
  * Made for the few rows of a draft tree: more than 32 rows are taken 32 at a time, each pass reading the weight. */

@@ -318,7 +318,8 @@ size_t moev_w4_packed_bytes(const moev_linear* p) {
 }
 
 moev_status moev_w4_pack(const moev_linear* p, const void* codes, const void* scales, void* packed, void* cuda_stream) {
-  if (!linear_ok(p) || !codes || !scales || !packed || !aligned(codes, 16) || !aligned(scales, 16) || !aligned(packed, 16)) return MOEV_EINVAL;
+  if (!linear_ok(p) || !codes || !scales || !packed || !aligned(codes, 4) || !aligned(packed, 16)) return MOEV_EINVAL;
+  if (!aligned(scales, p->wfmt == MOEV_W_INT4 ? 2 : 1)) return MOEV_EINVAL;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const int chunks = linear_chunks(p);
   const long long units = (long long)linear_tiles(p) * chunks;
