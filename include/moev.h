@@ -366,7 +366,8 @@ moev_status moev_add_rmsnorm(const moev_norm* p, void* cuda_stream);
  *   MOEV_W_MXFP4  codes uint8 [N, K / 2], scales uint8 [N, K / 32], group 32
  * codes on a 4-byte boundary.  K is a multiple of 32 and of group; N is free; MXFP4 scales lie between 2^-100 and 2^100.  moev_w4_pack lays a weight out
  * once in the order in which the kernel streams it (moev_w4_packed_bytes bytes, 16-byte aligned,
- * caller-owned); moev_linear_w4 reads the packed form.  Products are exact, sums are binary32; y is yfmt (moev_afmt).
+ * caller-owned); moev_linear_w4 reads the packed form.  Products are exact (MXFP4: of x held to 2^-40 of the largest of
+ * its 128 columns, where that is above 2^-111), sums are binary32; y is yfmt (moev_afmt).
  * Made for the few rows of a draft tree: more than 32 rows are taken 32 at a time, each pass reading the weight. */
 typedef struct {
   int32_t N, K, wfmt, group;
@@ -380,7 +381,12 @@ moev_status moev_linear_w4(const moev_linear* p, const void* packed, const float
  * one for V, positive, a power of two wherever moev_cache_append wrote it.
  *   k [n_pages, n_kv_heads, page, head_dim] e4m3      v [n_pages, n_kv_heads, head_dim, page] e4m3
  *   k_scale, v_scale [n_pages, n_kv_heads] float32
- * page is 16, 32, 64 or 128, head_dim 64 or 128. */
+ * page is 16, 32, 64 or 128, head_dim 64 or 128; k and v on 16-byte boundaries.
+ * Every slot below ctx_len counts as context for all drafts, in the order of the slots, and nothing here moves a token to
+ * another slot.  After a tree has been verified ctx_len may grow by the length of the accepted path where that is drafts 0, 1, 2,
+ * .. in this order (a chain, or the tree's first path).  Any other accepted path has to be written once more, as a chain: with
+ * moev_cache_append from the k and v that the caller kept, or by running the accepted tokens through the blocks again
+ * (moev_verify_blocks keeps k and v in no form but the cache's). */
 typedef struct {
   int32_t n_pages, page, n_kv_heads, head_dim;
   uint8_t *k, *v;
@@ -410,7 +416,8 @@ typedef struct {
  * given, are rotated in binary32; q_out (may be q) receives the queries in bf16.  A page's scale is the smallest power of
  * two that brings its largest magnitude to 448 or less; a page that held tokens before (ctx_len inside it) keeps
  * the larger of that and its old scale, and its tokens are rescaled when it grows.  The pages that receive tokens belong to
- * one sequence each.  A NaN stays NaN, an infinity becomes the largest finite value. */
+ * one sequence each.  A NaN stays NaN, an infinity becomes the largest finite value.  k, v, q, q_out and rope lie on 16-byte
+ * boundaries. */
 moev_status moev_cache_append(const moev_kv_cache* cache, const moev_draft_batch* batch, const void* k, int64_t k_stride,
                               const void* v, int64_t v_stride, const float* rope, int32_t rope_rows, const void* q,
                               int64_t q_stride, int32_t n_heads, void* q_out, int64_t q_out_stride, void* cuda_stream);
@@ -420,7 +427,8 @@ moev_status moev_cache_append(const moev_kv_cache* cache, const moev_draft_batch
  * A draft sees the context and, of the drafts, itself and its ancestors; with window > 0 of all these
  * only the last window positions (pages that end before ctx_len + 1 - window may have been given back: their entries in the
  * page table are not looked at).  scores are multiplied by scale (> 0); sinks [n_heads] float32 (or
- * NULL) join the denominator.  lse [n_tokens, n_heads] float32 (or NULL): natural log of the denominator.
+ * NULL) join the denominator.  lse [n_tokens, n_heads] float32 (or NULL): natural log of the denominator.  q and out lie on
+ * 16-byte boundaries.
  * Roundings: q is held to 2^-12 of an element or 2^-18 of its row's largest, whichever is more; scores, sums and lse are
  * binary32; a key's probability times its page's V scale is rounded once to 11 bits (2^-11), or by 2^-28 of the row's largest
  * such product of a key whose V is not all zero, whichever is more (V scales below 2^-48 of the sequence's largest: or
@@ -438,7 +446,7 @@ moev_status moev_cache_attend(const moev_kv_cache* cache, const moev_draft_batch
  *   x = norm(h, ffn_norm);   h += MoE(x)  (moev_verify with ctx)
  * and after the last one, where final_norm is given, final_out = norm(h, final_norm). */
 typedef struct {
-  const void *attn_norm, *ffn_norm; /* bfloat16 [H] */
+  const void *attn_norm, *ffn_norm; /* bfloat16 [H], 16-byte aligned as the other norm, hidden and final_out */
   moev_linear qkv, o;               /* [(n_heads + 2 n_kv_heads) head_dim, H] and [H, n_heads head_dim] */
   const void *qkv_packed, *o_packed;
   const float *qkv_bias, *o_bias;   /* or NULL */

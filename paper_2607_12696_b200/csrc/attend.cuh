@@ -37,10 +37,11 @@
 //
 // Bound, as measured on B200 (us; bytes at 6.5 TB/s and operations at 1.67 PFLOP/s allow the time in brackets): one draft, 16
 // rows, 4096 keys 13 (0.7): two launches, set-up, one tile and the join, each a chain of trips to memory; 64 drafts x 16
-// heads over 16 000 keys 130 (20): the softmax warps' instructions, 5 800 cycles a tile of 128 x 128, of which the tensor
-// core needs 1 800; 32 ragged sequences up to 24 000 keys, 32 rows 205 (121): 3 500 cycles a tile of 32 KB on either of an
-// SM's two CTAs, two thirds of the issue slots, 3.9 TB/s; window of 128, 64 rows, 16 sequences 17 (0.5): three masked
-// tiles a CTA.  The same work on mma.sync with the rows as the wide operand took 187 and 333 us for the second and third.
+// heads over 16 000 keys 130 (20): 28 tiles of 128 x 128 a CTA at 6 300 cycles each (90 us; the softmax warps' instructions, the
+// tensor core needs 1 800) and 40 us for the set-up of one or two pieces and the join; 32 ragged sequences up to 24 000 keys,
+// 32 rows 206 (121): 81 tiles of 32 KB on either of an SM's two CTAs at 3 250 cycles (134 us, 56 % of the issue slots) and 70 us
+// for set-up and join; window of 128, 64 rows, 16 sequences 17 (0.5): three masked tiles a CTA.  The same work on mma.sync
+// with the rows as the wide operand took 187 and 333 us for the second and third.
 #pragma once
 #include <cuda.h>
 

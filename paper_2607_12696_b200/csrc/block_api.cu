@@ -107,7 +107,9 @@ cudaError_t launch_linear(const w4::Args& a0, cudaStream_t st) {
   const int tiles = (a.N + 15) / 16;
   const int rows = std::min(a.n, 8 * NT), passes = (a.n + 8 * NT - 1) / (8 * NT);
   // All 16 warps of an SM share one copy of x.  kw of them share a tile's K: the fewest with which the tiles occupy
-  // most warps of the machine, never more than there are chunks.
+  // most warps (60 %) of the machine, never more than there are chunks.  Measured at 40 / 60 / 80 % (us): 1 row, 8192 -> 4096 9.9 / 6.7 /
+  // 6.6; 8 rows, 2880 -> 5120 MXFP4 8.1 / 7.7 / 7.7; 4 rows, 4096 -> 2880 MXFP4 6.4 / 6.4 / 7.0; 16 rows, 4096 -> 20000 25.3 / 23.3 / 23.4;
+  // 8 rows, 2880 -> 14000 10.3 / 10.3 / 10.9.
   const int warps = 16;
   int kw = 1;
   while (kw < 16 && 2 * kw <= a.n_chunks && tiles * kw * 10 < sms * warps * 6) kw *= 2;
@@ -190,6 +192,9 @@ Plan attend_plan(const moev_kv_cache* c, const moev_draft_batch* d, int n_heads,
   if (window > 0) span = std::min<long long>(span, (long long)window + d->max_drafts + att::kKeys - 1);
   const long long tiles = (span + att::kKeys - 1) / att::kKeys;  // of keys, at most
   const long long segments = (long long)d->n_seq * c->n_kv_heads * ((rows + p.rows - 1) / p.rows);
+  // Whole segments save the second kernel and set up once each, but leave CTAs empty where there are few of them.  Measured at
+  // 2 / 4 / 8 / 12 tiles, 8 kv heads, 8 rows each (us, whole | split): 16 sequences 11.5 | 14.7, 14.2 | 16.9, 19.1 | 21.2, 24.5 |
+  // 25.2; one sequence 10.9 | 11.6, 13.4 | 11.5, 17.6 | 11.5, 22.2 | 12.2.  Up to 4 tiles neither choice is far off.
   p.whole = tiles <= 4;
   p.units = segments * tiles;
   p.grid = (int)std::min<long long>(sm_count() * (p.rows <= 32 ? 2 : 1), p.whole ? segments : segments * tiles);
@@ -394,6 +399,8 @@ moev_status moev_cache_append(const moev_kv_cache* c, const moev_draft_batch* d,
   a.rep = q ? n_heads / c->n_kv_heads : 0;
   // pages that max_drafts tokens can touch, wherever the first one falls in its page
   const int pages = (d->max_drafts + c->page - 2) / c->page + 1;
+  // CTAs for a page's queries: one for up to 2 query heads per kv head, two above.  Measured with 1 / 2 / 3 (us): 2 heads, 4 096 tokens
+  // 20.0 / 21.2; 4 heads 25.5 / 24.7 / 25.7; 16 heads 60.8 / 56.2 / 52.5; 64 tokens, 8 heads 9.9 / 7.8 / 7.8.
   a.q_parts = std::min(2, (a.rep + 1) / 2);
   const int n_par = d->parent && rope ? std::min(d->max_drafts, kv::kMaxTree) : 0;
   const size_t smem = (size_t)(((c->page + n_par) * 4 + 15) & ~15) + (size_t)c->page * c->head_dim + (size_t)c->head_dim * (c->page + 4);

@@ -9,9 +9,11 @@
 //   MXFP4 in f16, where sign and magnitude of an e2m1 code are in place after one shift.  x is brought to f16 by a power of
 //   two per row and chunk of 128 k, its largest element to [2^14, 2^15), so that an element keeps all its 8 significant bits
 //   down to 2^-28 of the largest (and is off by at most 2^-40 of that below).
-// Bound by the weight stream (N K / 2 bytes + scales) at large N and by the instructions that unpack it: 16 rows, N = 100003,
-// K = 7168, groups of 64: 102 us for 387 MB, 3.8 TB/s, 0.58 of the copy rate, at 55 % of the issue slots.  1 row, N = 4096, K =
-// 8192: 6.6 us (18 MB, 2.7 us), 8 rows, N = 5120, K = 2880 MXFP4: 7.8 us (8 MB, 1.2 us), of which 1 to 2 us are set-up and staging.
+// 16 rows, N = 100003, K = 7168, groups of 64: 103 us in a graph, 112 us between other calls, for 387 MB (59 us): 3.5 to 3.8 TB/s, 55 %
+// of the issue slots, ALU and tensor pipe 43 % each: no pipe is full; what is left is latency with 16 warps an SM, and a third round
+// of tiles that is 64 % full.  1 row, N = 4096, K = 8192: 6.7 us (18 MB, 2.7 us), 8 rows, N = 5120, K = 2880 MXFP4: 7.8 us (8 MB,
+// 1.2 us), of which 1 to 2 us are set-up and staging.  More rows: x staged in pieces from about 28 rows of 4096 columns on, and one pass
+// over the weight per 32 rows: 5120 x 2880 MXFP4 8 / 16 / 32 / 64 / 128 rows 7.7 / 10.8 / 37 / 71 / 138 us.
 //
 // Packed layout (made once per weight, moev_w4_pack).  The weights are the A operand (16 outputs x
 // 16 k) and the tokens the B operand (8 columns), since a few tokens fill the narrow side.  A tile of
