@@ -83,7 +83,18 @@ class W4Linear:
                                 C.c_void_p(torch.cuda.current_stream().cuda_stream))
         if st != 0:
             raise MoevError(st, "moev_w4_pack rejected the weight")
-        self._args = (C.addressof(self._c), self.packed.data_ptr(), 0 if bias is None else bias.data_ptr(), dev)
+        self._address()
+
+    def _address(self):
+        self._args = (C.addressof(self._c), self.packed.data_ptr(), 0 if self.bias is None else self.bias.data_ptr(), self.packed.get_device())
+
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k not in ("_c", "_args")}
+
+    def __setstate__(self, state):  # a copy has addresses of its own
+        self.__dict__.update(state)
+        self._c = _Linear(self.N, self.K, self.wfmt, self.group)
+        self._address()
 
     def __call__(self, x: torch.Tensor, y: torch.Tensor = None) -> torch.Tensor:
         """moev_linear_w4: x bfloat16 [n, K] -> y bfloat16 or float32 [n, N] (allocated as bfloat16 when not given)."""
