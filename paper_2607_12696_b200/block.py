@@ -215,6 +215,12 @@ class Block:
                       self.qkv._args[2], self.o._args[2], _ptr(self.sinks), self.window, self.cache._c, self.layer)
 
 
+# outputs of the MoE layers beside y: type and least size for T token rows
+_DIAGNOSTICS = (("n_active", lambda c, T: 1, torch.int32), ("topk_ids", lambda c, T: T * c.top_k, torch.int32),
+                ("topk_w", lambda c, T: T * c.top_k, torch.float32), ("union_ids", lambda c, T: c.E, torch.int32),
+                ("offsets", lambda c, T: c.E + 1, torch.int32), ("perm", lambda c, T: T * c.top_k, torch.int32))
+
+
 def verify_blocks(verifier, blocks: list, batch: DraftBatch, hidden: torch.Tensor, n_heads: int, outs: list, rope: torch.Tensor = None,
                   eps: float = 1e-6, scale: float = None, final_norm: torch.Tensor = None, final_out: torch.Tensor = None,
                   workspace: torch.Tensor = None):
@@ -242,6 +248,11 @@ def verify_blocks(verifier, blocks: list, batch: DraftBatch, hidden: torch.Tenso
         _bad(f"final_norm, final_out: expected contiguous bfloat16 [{H}] and [{T}, {H}]")
     _same_device(hidden, batch.cu, rope, final_norm, final_out, workspace, *[o.get(f) for o in outs for f in _OUT_FIELDS],
                  *[t for b in blocks for t in (b.cache.k, b.attn_norm, b.ffn_norm, b.sinks, b.qkv.packed, b.o.packed)])
+    for o in outs:
+        for f, size, dtype in _DIAGNOSTICS:
+            t = o.get(f)
+            if t is not None and (t.dtype != dtype or t.numel() < size(verifier.cfg, T) or not t.is_contiguous()):
+                _bad(f"outs: {f} must be contiguous {dtype} of {size(verifier.cfg, T)} elements or more, got {tuple(t.shape)} {t.dtype}")
     if not hidden.is_cuda or hidden.get_device() != torch.cuda.current_device():
         _bad(f"tensors must be on the current CUDA device, got {hidden.device}")
     for o in outs:
