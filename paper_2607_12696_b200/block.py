@@ -241,6 +241,8 @@ def verify_blocks(verifier, blocks: list, batch: DraftBatch, hidden: torch.Tenso
         _bad(f"rope: expected contiguous float32 [positions, {D}]")
     if any(b.cache.head_dim != D for b in blocks):
         _bad("blocks with heads of different sizes need a call each")
+    if scale is not None and scale == 0.0:  # to the C entry point: no scale given
+        _bad("scale: expected a positive number")
     if (final_norm is None) != (final_out is None):
         _bad("final_norm and final_out go together")
     if final_norm is not None and (final_norm.dtype != torch.bfloat16 or final_norm.shape != (H,) or not final_norm.is_contiguous()

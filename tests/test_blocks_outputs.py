@@ -43,3 +43,8 @@ def test_outputs_that_fit_get_as_far_as_the_device():
     for out in (outputs(), {k: outputs()[k] for k in ("y", "n_active")}, {k: torch.cat([t, t]) for k, t in outputs().items()}):
         with pytest.raises(moev.MoevError, match="current CUDA device"):
             call(out)
+
+
+def test_a_scale_of_zero_is_no_scale():
+    with pytest.raises(moev.MoevError, match="scale"):
+        call(outputs(), scale=0.0)
