@@ -207,11 +207,12 @@ __global__ void __launch_bounds__(Cfg<D, T>::kThreads, 3 - T) prompt_kernel(cons
   };
   const int items = 2 * n_tiles - (MOEV_TEST_WITHHOLD() ? 1 : 0), fetched = min(items, C::kStages);
   if (warp == kLoader && lane == 0 && n_tiles > 0) {
+    // Q of the tiles that see keys: one that sees none waits for nothing, and its outputs change places where its Q would land
     const uint32_t q_bytes = (uint32_t)a.tile_heads * a.tokens * D * 2;
-    ptx::mbar_arrive_expect_tx(&S.q_full, q_bytes * (1 + (sp[1].tokens > 0)));
+    ptx::mbar_arrive_expect_tx(&S.q_full, q_bytes * ((to[0] > from[0]) + (to[1] > from[1])));
 #pragma unroll
     for (int t = 0; t < 2; ++t)
-      for (int h = 0; h < D / 64 && sp[t].tokens > 0; ++h)
+      for (int h = 0; h < D / 64 && to[t] > from[t]; ++h)
         ptx::tma_load_3d(smem + C::oQ + t * C::kQTile + h * C::kQHalf, &tm_q, &S.q_full, h * 64, head0, lo + sp[t].first, ptx::kPolicyEvictFirst);
 #pragma unroll 1
     for (int i = 0; i < fetched; ++i) load(i);

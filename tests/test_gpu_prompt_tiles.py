@@ -1,0 +1,63 @@
+"""Prompt attention in its form of two tiles of rows, at the masks that set its tiles apart, against float64.
+
+The host takes that form where the rows may see more than 700 keys (the smaller of the window and, with key rows of their own, all keys of the
+call, else the bound on the tokens) and there are too many CTAs for a cluster to share keys: hence the keys of no sequence and the
+empty sequences here."""
+import pytest
+import torch
+
+import paper_2607_12696_b200 as moev
+import prompt_ref as R
+
+pytestmark = pytest.mark.gpu
+BF16, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+EMPTY, SPARE = 160, 800
+
+
+def within(got, want, tol, what):
+    got, want = got.double().cpu(), want.cpu()
+    odd = ~torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), f"{what}: NaN in other places"
+    assert torch.equal(got[odd & ~torch.isnan(want)], want[odd & ~torch.isnan(want)]), f"{what}: other infinities"
+    over = ((got - want).abs() - tol)[~odd]
+    assert over.numel() == 0 or float(over.max()) <= 0, f"{what}: off by {float(over.max())} more than it may be"
+
+
+def starts(counts):
+    return [sum(counts[:b]) for b in range(len(counts) + 1)]
+
+
+def make(n_q, n_k, kv, rep, D, seed=0, empty=EMPTY):
+    """q, k, v on the host, offsets with empty sequences behind the others, rows of no sequence behind them."""
+    g = torch.Generator().manual_seed(seed)
+    cu, cu_k = starts(n_q), starts(n_k)
+    q, k, v = (torch.randn(*s, generator=g).to(BF16) for s in ((cu[-1] + 2, kv * rep, D), (cu_k[-1] + SPARE, kv, D), (cu_k[-1] + SPARE, kv, D)))
+    return q, k, v, cu + cu[-1:] * empty, cu_k + cu_k[-1:] * empty
+
+
+def run(q, k, v, cu, cu_k, most, repeats=1, **kw):
+    """out and lse, of buffers that held 7; the same bits every time."""
+    batch = moev.PromptBatch(torch.tensor(cu, dtype=I32, device="cuda"), most, cu_k=torch.tensor(cu_k, dtype=I32, device="cuda"))
+    dev, first = [t.cuda() for t in (q, k, v)], None
+    for _ in range(repeats):
+        out, lse = torch.full(q.shape, 7.0, dtype=BF16, device="cuda"), torch.full(q.shape[:2], 7.0, device="cuda")
+        moev.prompt_attend(batch, *dev, out, lse, **kw)
+        assert first is None or (torch.equal(out.view(torch.int16), first[0].view(torch.int16)) and torch.equal(lse.view(I32), first[1].view(I32)))
+        first = first or (out, lse)
+    return first
+
+
+def check(q, k, v, cu, cu_k, most, repeats=1, window=0, sinks=None, rows=slice(None)):
+    out, lse = run(q, k, v, cu, cu_k, most, repeats, window=window, sinks=None if sinks is None else sinks.cuda())
+    want, want_l, tol, tol_l = R.prompt(q, k, v, cu, cu_k, q.shape[2] ** -0.5, window, sinks, torch.full(q.shape, 7.0), torch.full(q.shape[:2], 7.0))
+    within(lse[rows], want_l[rows], tol_l[rows], "lse")
+    within(out[rows], want[rows], tol[rows], "out")
+    return out, lse
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q,n_k,kv,rep", [([257] * 8, [100] * 8, 1, 1), ([300, 20], [100, 900], 1, 1), ([150, 20, 90], [70, 0, 10], 2, 2), ([60], [25], 1, 5),
+                                            ([129, 256], [1, 0], 1, 1)])
+def test_tile_that_sees_nothing_beside_one_that_does(n_q, n_k, kv, rep, D):
+    """Fewer keys than tokens by a tile of rows and more: its outputs are 0 every time, whatever its queries are."""
+    check(*make(n_q, n_k, kv, rep, D, seed=rep), 1000, repeats=200)
