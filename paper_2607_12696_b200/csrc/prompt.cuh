@@ -128,6 +128,16 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// 16 bytes of shared memory that another warp may be replacing by the same values.
+__device__ __forceinline__ uint4 load_relaxed(const uint4* p) {
+  uint4 w;
+  asm volatile("ld.relaxed.cta.shared::cta.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(ptx::smem_u32(p)) : "memory");
+  return w;
+}
+__device__ __forceinline__ void store_relaxed(uint4* p, const uint4& w) {
+  asm volatile("st.relaxed.cta.shared::cta.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ptx::smem_u32(p)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+}
+
 // SPLIT: the CTAs of a cluster share the keys of a tile of rows; each leaves its normalised output and its lse in shared memory, and joins a
 // share of the rows from all of them.
 template <int D, int T, bool SPLIT>
@@ -379,14 +389,14 @@ __global__ void __launch_bounds__(Cfg<D, T>::kThreads, 3 - T) prompt_kernel(cons
       att::tmem_st(p_at, p);
       l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       if (!both.at(k0)) {
-        // what some row does not see must not reach it through p = 0
+        // what some row does not see must not reach it through p = 0; both tiles' warps see to that, the same values at the same places
         const int iv = v_item(j, n_tiles);
         ok = att::wait_warp(&S.full[iv % C::kStages], (iv / C::kStages) & 1, &S.abort, a.status, lane) && ok;
         uint4* v = reinterpret_cast<uint4*>(smem + C::oRing + (iv % C::kStages) * C::kTile);
         bool bad = false;
 #pragma unroll 4
         for (int z = tid & 255; z < C::kTile / 16 && ok; z += 256) {
-          const uint4 w = v[z];
+          const uint4 w = load_relaxed(v + z);
           uint32_t w4[4] = {w.x, w.y, w.z, w.w}, any = 0;
           // an exponent of ones carries into the bit above it
 #pragma unroll
@@ -399,11 +409,11 @@ __global__ void __launch_bounds__(Cfg<D, T>::kThreads, 3 - T) prompt_kernel(cons
             }
             if (k0 + (z & (C::kHalf / 16 - 1)) / 8 < keys) S.bad = 1;  // keys behind the sequence are nobody's
             __threadfence_block();
-            v[z] = make_uint4(w4[0], w4[1], w4[2], w4[3]);
+            store_relaxed(v + z, make_uint4(w4[0], w4[1], w4[2], w4[3]));
             bad = true;
           }
         }
-        if (bad) ptx::fence_proxy_async_smem();
+        if (T == 2 || bad) ptx::fence_proxy_async_smem();  // what it has read may be the other tile's doing, which this tile's product then reads
       }
       att::tmem_st_wait();
       ptx::tc_fence_before();

@@ -61,3 +61,29 @@ def check(q, k, v, cu, cu_k, most, repeats=1, window=0, sinks=None, rows=slice(N
 def test_tile_that_sees_nothing_beside_one_that_does(n_q, n_k, kv, rep, D):
     """Fewer keys than tokens by a tile of rows and more: its outputs are 0 every time, whatever its queries are."""
     check(*make(n_q, n_k, kv, rep, D, seed=rep), 1000, repeats=200)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,kv,rep,window", [(900, 1, 1, 705), (900, 1, 1, 0), (300, 2, 4, 0), (170, 1, 8, 0)])
+def test_both_tiles_hide_the_same_values(n, kv, rep, window, D):
+    """NaN and infinities in keys that come later, that the window has left behind, and of nobody: both tiles of rows clear the same shared tile of V."""
+    q, k, v, cu, cu_k = make([n, 40], [n, 40], kv, rep, D, seed=window)
+    for t in (k, v):
+        t[n - 20, 0, 3] = torch.nan
+        t[n - 5, 0, 40], t[n - 3, 0, 40] = torch.inf, -torch.inf
+        t[n + 40:] = torch.nan
+    if window:  # rows from 745 on see none of these; rows of the same tiles in front of them do
+        for t in (k, v):
+            t[20:40:5, 0, 7] = torch.nan
+            t[39, 0, 9] = torch.inf
+    rows = torch.zeros(q.shape[0], dtype=torch.bool)
+    rows[:20], rows[(745 if window else 20):n - 20], rows[n:n + 40] = True, True, True
+    check(q, k, v, cu, cu_k, 1000, repeats=50, window=window, rows=rows)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_values_that_one_of_two_tiles_sees_stay(D):
+    n = 400
+    q, k, v, cu, cu_k = make([n], [n], 1, 1, D, seed=3)
+    v[130, 0, 3], v[n - 9, 0, 5], v[n - 7, 0, 6], v[n - 5, 0, 6] = torch.inf, torch.nan, torch.inf, -torch.inf
+    check(q, k, v, cu, cu_k, 1000, repeats=50)
