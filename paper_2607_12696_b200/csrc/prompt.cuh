@@ -440,8 +440,6 @@ __global__ void __launch_bounds__(Cfg<D, T>::kThreads, 3 - T) prompt_kernel(cons
         if (l != 0.f) {
           inv *= att::exp2_fast(lse2 - ref) / all;
           lse2 = lse2 != lse2 ? lse2 : ref + att::log2_fast(all);
-        } else {
-          lse2 = sink;
         }
       }
       const int hq = head0 + head;
@@ -498,7 +496,8 @@ __global__ void __launch_bounds__(Cfg<D, T>::kThreads, 3 - T) prompt_kernel(cons
           const uint4 u = *reinterpret_cast<const uint4*>(turn + from_row * D + ((piece ^ (from_row & (kPieces - 1))) << 4));
           if (at >= 0) *reinterpret_cast<uint4*>(a.out + at + piece * 8) = u;
         }
-        if (live && a.lse && half == 0) a.lse[(long long)(lo + my.first + token) * a.n_heads + hq] = lse2 * 0.6931471805599453f;
+        if (live && a.lse && half == 0)  // (of a row that sees nothing the sink as it is given)
+          a.lse[(long long)(lo + my.first + token) * a.n_heads + hq] = l == 0.f && a.sinks ? a.sinks[hq] : lse2 * 0.6931471805599453f;
       }
     }
   }
@@ -521,13 +520,20 @@ __global__ void __launch_bounds__(Cfg<D, T>::kThreads, 3 - T) prompt_kernel(cons
             asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[p].x), "=f"(x[p].y), "=f"(x[p].z), "=f"(x[p].w) : "r"(at));
           }
         }
-        const float sink = a.sinks ? a.sinks[head0 + head] * 1.4426950408889634f : -INFINITY;
+        float lse = a.sinks ? a.sinks[head0 + head] : -INFINITY;  // that of a row that sees nothing
+        const float sink = lse * 1.4426950408889634f;
         float ref = sink, all = 0.f;
+        bool none = true;
 #pragma unroll
-        for (uint32_t p = 0; p < 8; ++p)
-          if (p < ranks) ref = fmaxf(ref, lse2[p]);
+        for (uint32_t p = 0; p < 8; ++p) {
+          if (p < ranks) {
+            ref = fmaxf(ref, lse2[p]);
+            none = none && lse2[p] == -INFINITY;
+          }
+        }
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (ref > -INFINITY) {
+        if (none) {
+        } else if (ref > -INFINITY) {
           all = att::exp2_fast(sink - ref);
 #pragma unroll
           for (uint32_t p = 0; p < 8; ++p) {
@@ -545,17 +551,16 @@ __global__ void __launch_bounds__(Cfg<D, T>::kThreads, 3 - T) prompt_kernel(cons
           o.y *= inv;
           o.z *= inv;
           o.w *= inv;
-        } else {  // nothing seen, or nothing but NaN
-#pragma unroll
-          for (uint32_t p = 0; p < 8; ++p)
-            if (p < ranks && lse2[p] != lse2[p]) o.x = o.y = o.z = o.w = all = lse2[p];
+          lse = (ref + att::log2_fast(all)) * 0.6931471805599453f;
+        } else {  // nothing but NaN
+          o.x = o.y = o.z = o.w = lse = __int_as_float(0x7fffffff);
         }
         const long long at = (long long)(lo + sp[0].first + token);
         const __nv_bfloat162 u = __floats2bfloat162_rn(o.x, o.y), v = __floats2bfloat162_rn(o.z, o.w);
         if (!S.abort)
           *reinterpret_cast<uint2*>(a.out + at * a.out_stride + (long long)(head0 + head) * D + piece * 4) =
               make_uint2(*reinterpret_cast<const uint32_t*>(&u), *reinterpret_cast<const uint32_t*>(&v));
-        if (a.lse && piece == 0) a.lse[at * a.n_heads + head0 + head] = all == 0.f ? -INFINITY : (ref + att::log2_fast(all)) * 0.6931471805599453f;
+        if (a.lse && piece == 0) a.lse[at * a.n_heads + head0 + head] = lse;
       }
     }
     cluster_sync();

@@ -87,3 +87,13 @@ def test_values_that_one_of_two_tiles_sees_stay(D):
     q, k, v, cu, cu_k = make([n], [n], 1, 1, D, seed=3)
     v[130, 0, 3], v[n - 9, 0, 5], v[n - 7, 0, 6], v[n - 5, 0, 6] = torch.inf, torch.nan, torch.inf, -torch.inf
     check(q, k, v, cu, cu_k, 1000, repeats=50)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q,n_k,kv,rep,window", [([5], [130], 1, 136, 0), ([9], [800], 1, 128, 0), ([30, 1, 17], [200, 400, 17], 1, 5, 0), ([20, 6], [12, 0], 2, 2, 0),
+                                                   ([120, 3], [900, 740], 1, 2, 705), ([200], [1100], 1, 3, 705)])
+def test_two_tiles_keys_of_their_own_windows_and_sinks(n_q, n_k, kv, rep, window, D):
+    q, k, v, cu, cu_k = make(n_q, n_k, kv, rep, D, seed=rep)
+    sinks = torch.randn(kv * rep, generator=torch.Generator().manual_seed(1))
+    check(q, k, v, cu, cu_k, 1000, window=window, sinks=sinks)
+    check(q, k, v, cu, cu_k, 1000, window=window)
