@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(Cfg<D, T>::kThreads, 3 - T) prompt_kernel(cons
       if (!SPLIT && a.sinks && live) {
         const float sink = a.sinks[head0 + head] * 1.4426950408889634f;
         // the larger of the two is the reference of their sum
-        const float ref = fmaxf(sink, lse2), all = att::exp2_fast(sink - ref) + att::exp2_fast(lse2 - ref);
+        const float ref = fmaxf(sink, lse2), all = (sink == ref ? 1.f : att::exp2_fast(sink - ref)) + att::exp2_fast(lse2 - ref);  // (an infinite sink is its own reference)
         if (l != 0.f) {
           inv *= att::exp2_fast(lse2 - ref) / all;
           lse2 = lse2 != lse2 ? lse2 : ref + att::log2_fast(all);
@@ -534,7 +534,7 @@ __global__ void __launch_bounds__(Cfg<D, T>::kThreads, 3 - T) prompt_kernel(cons
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         if (none) {
         } else if (ref > -INFINITY) {
-          all = att::exp2_fast(sink - ref);
+          all = sink == ref ? 1.f : att::exp2_fast(sink - ref);
 #pragma unroll
           for (uint32_t p = 0; p < 8; ++p) {
             if (p < ranks && lse2[p] != -INFINITY) {  // (a part without keys has no output either)
