@@ -199,7 +199,7 @@ moev_status moev_prompt_attend(const moev_prompt_batch* b, const moev_prompt* p,
   a.tile_heads = std::min(a.rep, prm::kRows);
   a.groups = (a.rep + a.tile_heads - 1) / a.tile_heads;
   a.tokens = prm::kRows / a.tile_heads;
-  a.window = p->window;
+  a.window = p->window < b->n_keys ? p->window : 0;  // one that no sequence fills hides nothing; position - window stays inside 32 bits
   // Small CTAs, two on an SM, where a row's keys are few: their beginnings and ends then weigh as much as what is between.  Us, small | large: 30 tokens
   // x 200 61 | 78, 300 x 100 277 | 298, 700 x 1 17.1 | 18.3, 800 x 60 544 | 547, 1000 x 8 112 | 109, 2000 x 1 56 | 48; window 128 118 | 132, 512 236 | 242,
   // 1000 94 | 87 (4 to 8 kv heads, 8 or 16 query heads each, D 128).
