@@ -503,7 +503,8 @@ typedef struct {
  * What a row does not see does not reach it, NaN and infinity included.  out overlaps none of the inputs.
  * Rotary positions: moev_cache_append rotates any heads that it is given as q; with q the [query heads | key heads] columns of a fused
  * projection (n_heads + n_kv_heads of them), q_out holds the rotated queries and keys for this call, next to the cache's own.
- * Roundings: scores, sums and lse are binary32, a probability is rounded once to bfloat16 for the product with v. */
+ * Roundings: scores, sums and lse are binary32, a probability is rounded once to bfloat16 for the product with v.  Sums are taken
+ * before they are divided: 2^8 times the sum of the |v| that a row sees has to stay below 2^128. */
 typedef struct {
   int32_t n_heads, n_kv_heads, head_dim, window;
   float scale;

@@ -10,8 +10,8 @@
 // V stays as it lies in memory ([key][d], its N contiguous).  A softmax thread has half of a row's keys of a tile (with two warps
 // for 32 rows there are four on each scheduler to hide their latencies); the halves meet once a tile.  p is rounded once to bf16 (half a
 // step 2^-8 relative at most, the type of v and out); maxima, denominators and O are binary32.  The reference of the exponentials is the maximum of the
-// first tile that a row sees; P, O and the denominators have binary32's range, so it moves (and O is rescaled) only when a
-// row's maximum has grown by more than 2^60.
+// first tile that a row sees; it moves (and O is rescaled) only when p has grown beyond 2^8, which is rare and leaves O the range
+// of binary32 but for a factor of 2^8: the sum of 2^8 |v| over the keys of a row has to stay below 2^128.
 //
 // Tensor memory, 512 columns at D = 128: one S (128), P of both tiles (64 each), O of both (128 each).  S is free as soon as it has been
 // read into registers: S of the one tile is computed while the other's softmax is under way, the products with V in between, and
@@ -41,7 +41,7 @@ namespace moev {
 namespace prm {
 
 constexpr int kRows = 128;
-constexpr float kSlack = 60.f;  // the maximum may grow by 2^60 before the reference follows
+constexpr float kSlack = 8.f;  // p may grow to 2^8 before the reference follows
 constexpr unsigned long long kBudgetNs = kDeviceWaitBudgetNs;
 
 struct Args {
