@@ -107,7 +107,7 @@ moev_status linear_i8(const moev_w8* p, const int8_t* x, int64_t x_stride, const
   if (n <= 16) return done(launch_few<16>(a, x, x_stride, p->w, p->K, st));
   if (n <= 32) return done(launch_few<32>(a, x, x_stride, p->w, p->K, st));
   if (n <= 64) return done(launch_few<64>(a, x, x_stride, p->w, p->K, st));
-  a.wide_tiles = (n + 255) / 256;
+  a.wide_tiles = (n - 1) / 256 + 1;
   a.narrow_tiles = (p->N + i8::kWide - 1) / i8::kWide;
   const long long tiles = (long long)a.wide_tiles * a.narrow_tiles;
   // tiles of a quarter of the size and a shared K where the large ones would leave two thirds of the SMs empty (us, large | small: 200 x 2000 -> 1000
