@@ -294,7 +294,7 @@ moev_status moev_build_pages(const moev_pages* p, void* cuda_stream) {
   const int chunks = std::max(1, (p->n_seq + pages::kChunk - 1) / pages::kChunk);
   // CTAs that share a chunk's rows: about 4 rows a thread, no more CTAs than two per SM
   const int rows = p->slots || p->positions ? p->n_tokens : 0;
-  a.parts = std::max(1, std::min(2 * sm_count() / chunks, (rows / chunks + 4 * pages::kChunk - 1) / (4 * pages::kChunk)));
+  a.parts = std::max(1, std::min(2 * sm_count() / chunks, rows / chunks / (4 * pages::kChunk) + 1));
   return done(launch(pages::pages_kernel, dim3(chunks * a.parts), dim3(pages::kChunk), 0, static_cast<cudaStream_t>(cuda_stream), a));
 }
 

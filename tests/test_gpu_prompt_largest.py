@@ -29,3 +29,23 @@ def test_linear_of_the_most_rows(n):
     for at in ends:
         y[at] = 0
     assert int(torch.count_nonzero(y)) == 0
+
+
+def test_pages_of_the_most_rows():
+    """Rows of no sequence up to the last one; as many CTAs as a call of a few rows less takes, so at the same pace (one CTA alone: a hundred times slower)."""
+    t = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    ms = {}
+    for n in (MOST - 4096, MOST):
+        out = {"cu": t([0, 0]), "positions": torch.full((n,), 7, dtype=torch.int32, device="cuda")}
+        ms[n] = []
+        for _ in range(3):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            moev.build_pages(t([5]), t([9]), t([[3]]), t([1]), 16, out)
+            b.record()
+            b.synchronize()
+            ms[n].append(a.elapsed_time(b))
+        pos = out.pop("positions")
+        assert pos[:10].tolist() == list(range(5, 14)) + [-1] and int(torch.count_nonzero(pos[9:] + 1)) == 0
+        del pos
+    assert min(ms[MOST]) < 4 * min(ms[MOST - 4096]), ms
