@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(Cfg<D, T>::kThreads, 3 - T) prompt_kernel(cons
         bool bad = false;
 #pragma unroll 4
         for (int z = tid & 255; z < C::kTile / 16 && ok; z += 256) {
-          const uint4 w = load_relaxed(v + z);
+          const uint4 w = T == 2 ? load_relaxed(v + z) : v[z];
           uint32_t w4[4] = {w.x, w.y, w.z, w.w}, any = 0;
           // an exponent of ones carries into the bit above it
 #pragma unroll
@@ -409,7 +409,9 @@ __global__ void __launch_bounds__(Cfg<D, T>::kThreads, 3 - T) prompt_kernel(cons
             }
             if (k0 + (z & (C::kHalf / 16 - 1)) / 8 < keys) S.bad = 1;  // keys behind the sequence are nobody's
             __threadfence_block();
-            store_relaxed(v + z, make_uint4(w4[0], w4[1], w4[2], w4[3]));
+            const uint4 clean = make_uint4(w4[0], w4[1], w4[2], w4[3]);
+            if (T == 2) store_relaxed(v + z, clean);
+            else v[z] = clean;
             bad = true;
           }
         }
@@ -520,20 +522,13 @@ __global__ void __launch_bounds__(Cfg<D, T>::kThreads, 3 - T) prompt_kernel(cons
             asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[p].x), "=f"(x[p].y), "=f"(x[p].z), "=f"(x[p].w) : "r"(at));
           }
         }
-        float lse = a.sinks ? a.sinks[head0 + head] : -INFINITY;  // that of a row that sees nothing
-        const float sink = lse * 1.4426950408889634f;
+        const float sink_in = a.sinks ? a.sinks[head0 + head] : -INFINITY, sink = sink_in * 1.4426950408889634f;
         float ref = sink, all = 0.f;
-        bool none = true;
 #pragma unroll
-        for (uint32_t p = 0; p < 8; ++p) {
-          if (p < ranks) {
-            ref = fmaxf(ref, lse2[p]);
-            none = none && lse2[p] == -INFINITY;
-          }
-        }
+        for (uint32_t p = 0; p < 8; ++p)
+          if (p < ranks) ref = fmaxf(ref, lse2[p]);
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (none) {
-        } else if (ref > -INFINITY) {
+        if (ref > -INFINITY) {
           all = sink == ref ? 1.f : att::exp2_fast(sink - ref);
 #pragma unroll
           for (uint32_t p = 0; p < 8; ++p) {
@@ -551,16 +546,22 @@ __global__ void __launch_bounds__(Cfg<D, T>::kThreads, 3 - T) prompt_kernel(cons
           o.y *= inv;
           o.z *= inv;
           o.w *= inv;
-          lse = (ref + att::log2_fast(all)) * 0.6931471805599453f;
-        } else {  // nothing but NaN
-          o.x = o.y = o.z = o.w = lse = __int_as_float(0x7fffffff);
+        } else {  // nothing seen, or nothing but NaN
+#pragma unroll
+          for (uint32_t p = 0; p < 8; ++p)
+            if (p < ranks && lse2[p] != lse2[p]) o.x = o.y = o.z = o.w = all = lse2[p];
         }
         const long long at = (long long)(lo + sp[0].first + token);
         const __nv_bfloat162 u = __floats2bfloat162_rn(o.x, o.y), v = __floats2bfloat162_rn(o.z, o.w);
         if (!S.abort)
           *reinterpret_cast<uint2*>(a.out + at * a.out_stride + (long long)(head0 + head) * D + piece * 4) =
               make_uint2(*reinterpret_cast<const uint32_t*>(&u), *reinterpret_cast<const uint32_t*>(&v));
-        if (a.lse && piece == 0) a.lse[at * a.n_heads + head0 + head] = lse;
+        if (a.lse && piece == 0) {
+          bool none = true;  // then the sink as it is given
+#pragma unroll
+          for (uint32_t p = 0; p < 8; ++p) none = none && (p >= ranks || lse2[p] == -INFINITY);
+          a.lse[at * a.n_heads + head0 + head] = none ? sink_in : (ref + att::log2_fast(all)) * 0.6931471805599453f;
+        }
       }
     }
     cluster_sync();
