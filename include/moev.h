@@ -486,7 +486,9 @@ moev_status moev_verify_blocks(moev_ctx* ctx, int32_t n_blocks, const moev_block
 
 /* Packed prompts.  Sequence b has the token rows cu[b] .. cu[b+1] - 1 and the key rows cu_k[b] .. cu_k[b+1] - 1; its tokens are the
  * last of its keys: token i stands at position keys - tokens + i (below 0, where there are fewer keys than tokens, it sees nothing).
- * cu_k NULL: cu, and n_keys = n_tokens.  max_tokens >= every sequence's tokens sizes the launch.  A sequence that breaks
+ * cu_k NULL: cu, and n_keys = n_tokens.  max_tokens >= every sequence's tokens, and 1 at least, sizes
+ * the launch (n_seq * max_tokens rows of tokens, whether they are there or not: one long prompt among many short ones is better a call
+ * of its own).  A sequence that breaks
  * the bounds is left out and raises *status (may be NULL) to 1; 4: a bounded wait ran out, outputs are undefined.  Rows that belong to
  * no sequence are left as they are. */
 typedef struct {
@@ -498,9 +500,9 @@ typedef struct {
 /* Causal attention over packed prompts.  q, out bfloat16 [n_tokens, n_heads * head_dim], k, v bfloat16 [n_keys, n_kv_heads *
  * head_dim], row strides multiples of 8 elements, on 16-byte boundaries; query head h reads kv head h / (n_heads / n_kv_heads);
  * head_dim 64 or 128.  A token sees the keys of its sequence up to its own position, with window > 0 only the last window of
- * those.  Scores are multiplied by scale (> 0); sinks [n_heads] float32 (or NULL) join the denominator.  lse [n_tokens, n_heads]
- * float32 (or NULL): natural log of the denominator.  A row that sees nothing has output 0 and lse -infinity (or the sink's).
- * What a row does not see does not reach it, NaN and infinity included.  out overlaps none of the inputs.
+ * those.  Scores are multiplied by scale (> 0); sinks [n_heads] float32 (or NULL) join the denominator (an infinite one leaves the keys nothing).  lse [n_tokens, n_heads]
+ * float32 (or NULL): natural log of the denominator.  A row that sees nothing has output 0 and lse -infinity (or the
+ * sink as it is given).  What a row does not see does not reach it, NaN and infinity included.  out overlaps none of the inputs.
  * Rotary positions: moev_cache_append rotates any heads that it is given as q; with q the [query heads | key heads] columns of a fused
  * projection (n_heads + n_kv_heads of them), q_out holds the rotated queries and keys for this call, next to the cache's own.
  * Roundings: scores, sums and lse are binary32, a probability is rounded once to bfloat16 for the product with v.  Sums are taken
@@ -541,7 +543,7 @@ size_t moev_linear_w8_workspace(const moev_w8* p, int32_t n);
 moev_status moev_linear_w8(const moev_w8* p, const void* x, int64_t x_stride, int32_t xfmt, int32_t n, void* y, int64_t y_stride, int32_t yfmt,
                            void* workspace, size_t workspace_bytes, void* cuda_stream);
 
-/* Log probabilities under rows of logits z [n, V] (afmt, row stride `stride`), l = scale * z (scale > 0: one over the temperature):
+/* Log probabilities under rows of logits z [n, V] (afmt, row stride `stride`; n up to 2^27, V to 2^30), l = scale * z (scale > 0: one over the temperature):
  *   lse = log sum_v exp(l_v)     logprobs[i, j] = l[ids[i, j]] - lse     entropy = lse - sum_v p_v l_v
  *   top_ids[i, 0..k-1]: the k largest z of the row, descending, ties to the lower id; top_logprobs: theirs
  * ids [n, m] int32: an id outside the vocabulary (padding) has -infinity.  ids and logprobs are given exactly with m > 0, top_ids exactly

@@ -14,8 +14,8 @@
 // among the CTAs of a cluster, so that all SMs stream the weight; the CTAs add each other's integer sums through distributed
 // shared memory, each for its share of the tokens.
 //
-// Measured, x to codes included: 8001 x 7168 -> 9217 445 us (product 336 to 380, 2.8 to 3.1 POP/s, the tensor pipe 88 % busy: the
-// power limit; codes 34 to 45: 5.0 TB/s alone, issue slots next); 1 x 8192 -> 4096 8.5 us (weight 5.1 at the copy rate; a launch, the ring's first fill
+// Measured, x to codes included: 8001 x 7168 -> 9217 433 to 457 us call after call, 360 on a GPU that has rested for seconds (2.9 POP/s, the tensor pipe
+// 88 % busy: the power limit; codes 34 to 45 of it: 5.0 TB/s alone, issue slots next); 1 x 8192 -> 4096 8.5 us (weight 5.1 at the copy rate; a launch, the ring's first fill
 // and the cluster's sums are the rest), 1 x 4096 -> 60000 39 us (6.3 TB/s); 50 x 2880 -> 5120 9.4 us.
 #pragma once
 #include <cuda.h>
@@ -211,7 +211,7 @@ struct Args {
   int n, N, steps;  // tokens, channels, steps of K
   int y_f32;
   int early;        // the kernel in front brings x to codes: the weight can be fetched before it has ended
-  int wide_tiles, narrow_tiles;  // tiles of 128 (M side) and of the other side
+  int wide_tiles, narrow_tiles;  // tiles of 256 tokens, of 256 channels
   const void* x;                 // rows that few_kernel brings to codes itself
   long long x_stride;
   int K;

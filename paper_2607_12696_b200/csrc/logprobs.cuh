@@ -8,13 +8,14 @@
 // lowest values is as good as any other.  z of -infinity counts nothing; NaN and +infinity make all of a row's numbers NaN.
 //
 // The k largest come from the threads' maxima: with T the k-th largest of the maxima of groups of 4 threads, k values or more are not
-// below T, and they lie in groups whose maximum is not.  Only those groups (k of 128, hardly more) are read again, a warp a group;
+// below T, and they lie in groups whose maximum is not.  Only those groups (hardly more than k of the 128, 64 or 32 that 512, 256 or 128 threads make: with 32 groups and
+// k = 32 every one) are read again, a warp a group;
 // what is not below T gets its rank by counting.  Where more than fit are equal, the warps keep sorted lists of k
 // instead (ties go to the lowest id in either way).
 //
-// Measured: 4096 x 100003 binary32 240 us without alternatives (6.8 TB/s: memory), 8 of them 295, 32 376 (the second reading of the groups, rows'
+// Measured: 4096 x 100003 binary32 240 us without alternatives (6.8 TB/s: memory), 8 of them 295 to 303, 32 376 (the second reading of the groups, rows'
 // ends that no other row's loads cover); 64 x 151937 bf16, 5 of them 11.6 us (9 without): 3 us to read, the rest is latency, the joins
-// (barriers) and the second reading; one row of 100003, 20 of them 8.4 us on a cluster of 8 (5.1 without).
+// (barriers) and the second reading; one row of 100003, 20 of them 8.7 us on a cluster of 8 (5.1 without).
 #pragma once
 #include "common.cuh"
 

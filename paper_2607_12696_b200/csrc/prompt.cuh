@@ -25,9 +25,10 @@
 // registers: with a test of the lane instead an MMA took 115 cycles to issue, 64 to run), eight warps per tile do its softmax.  Every wait
 // is bounded.
 //
-// Measured (32 query heads, 4 kv heads, D 128): 16 000 tokens 1.59 ms (1.32 PFLOP/s, 0.79 of a large matrix product's rate) on a GPU that has
-// rested, 1.85 ms call after call (the power limit).  What bounds it: two products of 256 cycles each per 128 x 128 scores beside 1024 cycles of
-// exponentials (16 a cycle), which two tiles in turn share: tensor pipe and special functions 55 % busy each over a whole call of 4000 tokens, issue slots 54 %.
+// Measured (32 query heads, 4 kv heads, D 128): 16 000 tokens 1.58 ms (1.33 PFLOP/s, 0.80 of a large matrix product's rate) on a GPU that has
+// rested for seconds, 1.81 to 1.85 ms call after call (the power limit).  What bounds it: two products of 512 cycles each per 128 x 128 scores beside
+// 1024 cycles of exponentials (16 a cycle), which two tiles in turn share: tensor pipe and special functions 54 % busy each over a whole call of 4000 tokens,
+// issue slots 54 %.
 // Other splits that were slower: scores of 64 keys beside P, 870 to 990 TFLOP/s (an MMA that is 64 wide takes 52 cycles, not 32); a quarter of the
 // exponentials as polynomials on the FMA pipe, 1082 for 1184 (registers and issue slots); persistent CTAs that draw their tiles (87 KB of code,
 // spills: no better in any case but ragged batches, 500 us for 562, which the output's way through shared memory gave as well: 495).  The first loads begin

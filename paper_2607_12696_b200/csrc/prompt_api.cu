@@ -111,7 +111,8 @@ moev_status linear_i8(const moev_w8* p, const int8_t* x, int64_t x_stride, const
   a.narrow_tiles = (p->N + i8::kWide - 1) / i8::kWide;
   const long long tiles = (long long)a.wide_tiles * a.narrow_tiles;
   // tiles of a quarter of the size and a shared K where the large ones would leave two thirds of the SMs empty (us, large | small: 200 x 2000 -> 1000
-  // 16.3 | 9.3, 512 x 4096 -> 2880 20.3 | 18.9, 256 x 2880 -> 5120 19.2 | 21.0, 400 rows 20.7 | 26.6, 257 x 7168 -> 9000 35 | 47)
+  // 16.3 | 9.3, 512 x 4096 -> 2880 20.3 | 18.9, 400 x 2880 -> 5120 20.7 | 26.6, 257 x 7168 -> 9000 35 | 47; 256 x 2880 -> 5120 19.2 | 21.0, which lies
+  // just inside the border and takes the small ones)
   if (n <= 128 || (n < 65536 && 6 * tiles <= sm_count())) return done(launch_few<128>(a, x, x_stride, p->w, p->K, st));
   if (tiles > 0x3fffffff) return MOEV_EINVAL;
   CUtensorMap tx, tw;
@@ -202,11 +203,12 @@ moev_status moev_prompt_attend(const moev_prompt_batch* b, const moev_prompt* p,
   a.window = p->window < b->n_keys ? p->window : 0;  // one that no sequence fills hides nothing; position - window stays inside 32 bits
   // Small CTAs, two on an SM, where a row's keys are few: their beginnings and ends then weigh as much as what is between.  Us, small | large: 30 tokens
   // x 200 61 | 78, 300 x 100 277 | 298, 700 x 1 17.1 | 18.3, 800 x 60 544 | 547, 1000 x 8 112 | 109, 2000 x 1 56 | 48; window 128 118 | 132, 512 236 | 242,
-  // 1000 94 | 87 (4 to 8 kv heads, 8 or 16 query heads each, D 128).
+  // 1000 94 | 87 (4 to 8 kv heads, 8 or 16 query heads each, D 128).  With keys of their own the host knows no sequence's number of them, only that of
+  // the call: many short sequences beyond 700 keys together take the large CTAs too (100 of 30 tokens over 100 keys: 28.6 us, with a window of 100 26.8).
   const int span = std::min(p->window > 0 ? p->window : INT_MAX, b->cu_k ? b->n_keys : b->max_tokens), tokens = std::min(b->max_tokens, b->n_tokens);
   // Few rows over many keys: a cluster shares the keys of a small CTA's rows, as long as there are fewer than two CTAs per SM and each has two tiles
-  // of keys on the average (which is a matter of time only).  Us, shared | not: 1 token behind 4000 15.0 | 48, 50 behind 4000 21 | 59, 50 behind
-  // 1000 14.8 | 23.5, 16 behind 16000 38 | 169, 200 behind 4000 33 | 60; but 300 tokens alone 17.6 | 11.5.
+  // of keys on the average (which is a matter of time only).  Us, shared | not: 1 token behind 4000 14.0 | 48, 50 behind 4000 19.6 | 59, 50 behind
+  // 1000 14.8 | 23.5, 16 behind 16000 36.9 | 169, 200 behind 4000 31.7 | 60; but 300 tokens alone 17.6 | 10.4.
   const long long small = ((long long)tokens + a.tokens - 1) / a.tokens * a.kv_heads * a.groups * a.n_seq;
   const int keys = (int)std::min<long long>(p->window > 0 ? (long long)p->window + a.tokens : INT_MAX, b->cu_k ? b->n_keys / b->n_seq : b->max_tokens / 2);
   int ranks = 1;
